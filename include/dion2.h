@@ -402,6 +402,125 @@ int dion2_plan_form(int batch, int64_t rows, int64_t cols, float alpha,
                     int axis, int ns_steps, const dion2_options* opt,
                     int* form_out, int* chain_out, int* fused_out);
 
+/* ---- The layers around the step ------------------------------------------
+ * The passes of a linear layer y = W x + b and of layer norm that consume W
+ * and produce the G that the step takes. W and G have the step's layout:
+ * row-major, contiguous [rows][cols] = [fan-out][fan-in], 16-byte aligned.
+ * Activations are row-major [tokens][width] with unit stride along a row and
+ * a pitch (elements between rows) of their own; any alignment of whole
+ * elements will do. tokens may be 0: outputs of that many rows are not
+ * touched, and gradients of parameters are sums of nothing.
+ *
+ * Numerical contract:
+ *   - Every sum (products, means, column sums) is held in fp32 and an output
+ *     is rounded once, to nearest even, from it. Products of bf16 operands
+ *     run on bf16 MFMA (exact products), those of fp32 operands on fp32 MFMA.
+ *   - Sums are taken in an order fixed by the sizes, the type and whether
+ *     pointers and pitches allow 16-byte loads: runs repeat bitwise. No atomics.
+ *   - Activations are evaluated in fp32, Phi within 1e-6 relative for |z| <= 4
+ *     (4e-6 for |z| <= 9) in fp32 calls and 1e-5 in bf16 ones, from Z's sums
+ *     before rounding in dion2_linear_forward and from the stored Z in the
+ *     gradients. An infinite z gives what the formula gives (gelu(+inf) = inf,
+ *     gelu(-inf) = NaN). A NaN or infinity reaches the outputs whose sums it
+ *     is part of and no others.
+ *
+ * Conventions beyond those above: an output must not overlap an input or
+ * another output (DION2_ERR_INVALID_ARG), except that where an entry point
+ * says so it may be exactly the same matrix (pointer and pitch). Column
+ * slices of one buffer with equal pitches do not overlap. The stream's
+ * device must be the current one. Limits: 0 <= tokens < 2^31, rows and cols as
+ * for the step, pitches below 2^28, and tokens / 128 times the longer of rows
+ * and cols / 128 below 2^24 (DION2_ERR_UNSUPPORTED otherwise). Calls may be captured in a HIP graph; one that
+ * needs a workspace (dion2_linear_workspace_size,
+ * dion2_layernorm_workspace_size) then needs the caller's, since a graph
+ * may be replayed while the library's is in use or has been moved:
+ * DION2_ERR_WORKSPACE otherwise. Calls that share a caller's workspace must be
+ * ordered. */
+typedef enum dion2_act {
+    DION2_ACT_NONE = 0,
+    DION2_ACT_RELU = 1,       /* max(z, 0); slope 0 at 0                       */
+    DION2_ACT_GELU = 2,       /* z Phi(z), Phi the normal distribution function */
+    DION2_ACT_GELU_TANH = 3,  /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
+    DION2_ACT_SILU = 4        /* z / (1 + exp(-z))                              */
+} dion2_act;
+
+/* Options of the layer calls. Fill with dion2_layer_options_init; opt == NULL
+   means defaults. A call ignores the fields it does not name. */
+typedef struct dion2_layer_options {
+    int dtype;               /* W and all activations (default DION2_DTYPE_BF16)  */
+    int p_dtype;             /* bias, gamma, beta (default DION2_DTYPE_BF16)      */
+    int g_dtype;             /* G, dbias, dgamma, dbeta (default DION2_DTYPE_BF16) */
+    int act;                 /* dion2_act (default DION2_ACT_NONE)                */
+    int accumulate;          /* nonzero: gradients of parameters are added to what
+                                their outputs hold (read and rounded in g_dtype)  */
+    float eps;               /* layer norm's, >= 0 (default 1e-5)                 */
+    int64_t ld_x, ld_y, ld_z, ld_r;     /* pitches of X, Y, Z, R;                 */
+    int64_t ld_dx, ld_dy, ld_dz, ld_dr; /* of dX, dY, dZ, dR (0 = contiguous)     */
+    void* workspace;         /* DEVICE scratch, 256-B aligned, or NULL for the
+                                library-managed one                               */
+    size_t workspace_bytes;
+} dion2_layer_options;
+
+void dion2_layer_options_init(dion2_layer_options* opt);
+
+/* Y = act(X W^T + bias) + R.  X [tokens][cols], Y [tokens][rows]; optional:
+   bias [rows], R [tokens][rows] (the residual; may be Y itself), and the output
+   Z [tokens][rows] = X W^T + bias, the pre-activation that the gradients take.
+   Reads dtype, p_dtype, act, ld_x, ld_y, ld_z, ld_r. */
+int dion2_linear_forward(void* Y, const void* X, const void* W, const void* bias,
+                         const void* R, void* Z, int64_t tokens, int64_t rows,
+                         int64_t cols, const dion2_layer_options* opt, void* stream);
+
+/* dX = (dY W) .* act'(Z).  dY [tokens][rows], dX [tokens][cols]. Z [tokens][cols]
+   is the pre-activation of the layer whose activation X was, X = act(Z), so
+   that dX is that layer's gradient before its activation; NULL with
+   DION2_ACT_NONE. dX may be Z itself. Reads dtype, act, ld_dx, ld_dy, ld_z. */
+int dion2_linear_backward_input(void* dX, const void* dY, const void* W, const void* Z,
+                                int64_t tokens, int64_t rows, int64_t cols,
+                                const dion2_layer_options* opt, void* stream);
+
+/* G = dY^T X and dbias = sum over tokens of dY, or those added to G and dbias
+   (accumulate). G [rows][cols] is what the step takes; G or dbias may be
+   NULL (X too, without G). Reads dtype, g_dtype, accumulate, ld_dy, ld_x. */
+int dion2_linear_backward_weight(void* G, void* dbias, const void* dY, const void* X,
+                                 int64_t tokens, int64_t rows, int64_t cols,
+                                 const dion2_layer_options* opt, void* stream);
+
+/* dZ = dY .* act'(Z), all [tokens][width]: an activation's gradient where no
+   product follows it. dZ may be dY or Z itself. Reads dtype, act, ld_dz,
+   ld_dy, ld_z. */
+int dion2_activation_backward(void* dZ, const void* dY, const void* Z, int64_t tokens,
+                              int64_t width, const dion2_layer_options* opt, void* stream);
+
+/* Y = (X - mean) rstd gamma + beta per row, mean and rstd = 1 / sqrt(var + eps)
+   of that row's cols entries (var is the mean square deviation). gamma and
+   beta [cols] may be NULL (1 and 0); mean and rstd, fp32 [tokens], are optional
+   outputs. Y may be X itself. Reads dtype, p_dtype, eps, ld_x, ld_y. */
+int dion2_layernorm_forward(void* Y, float* mean, float* rstd, const void* X,
+                            const void* gamma, const void* beta, int64_t tokens,
+                            int64_t cols, const dion2_layer_options* opt, void* stream);
+
+/* With h = dY gamma and xh = (X - mean) rstd:
+     dX = rstd (h - mean(h) - xh mean(h xh)) + dR,
+     dgamma = sum over tokens of dY xh, dbeta = sum over tokens of dY
+   (added to what dgamma and dbeta hold with accumulate). mean and rstd are the
+   forward pass's. gamma may be NULL (1), dR (the gradient that reaches X past
+   the norm, along the residual) too, and any of the outputs but not all. dX
+   may be dY, X or dR itself. Reads dtype, p_dtype, g_dtype, accumulate, ld_dx,
+   ld_dy, ld_x, ld_dr. */
+int dion2_layernorm_backward(void* dX, void* dgamma, void* dbeta, const void* dY,
+                             const void* X, const float* mean, const float* rstd,
+                             const void* gamma, const void* dR, int64_t tokens,
+                             int64_t cols, const dion2_layer_options* opt, void* stream);
+
+/* Bytes of workspace that suffice for every linear call (every norm call) of
+   these sizes with opt's dtype, whatever the pitches; 0 where none is needed
+   or the sizes or types are invalid. */
+size_t dion2_linear_workspace_size(int64_t tokens, int64_t rows, int64_t cols,
+                                   const dion2_layer_options* opt);
+size_t dion2_layernorm_workspace_size(int64_t tokens, int64_t cols,
+                                      const dion2_layer_options* opt);
+
 /* ---- Measurement hooks ---------------------------------------------------
  * While enabled, every kernel phase of subsequent calls is bracketed by HIP
  * events recorded on the call's stream (the Newton-Schulz s x s products of

@@ -36,12 +36,19 @@ SELECT_L1, SELECT_RANDOM = 0, 1
 
 MAX_NS_STEPS = 16
 
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
+ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH,
+               "silu": ACT_SILU}
+
 # Every function include/dion2.h declares (checked by the ABI tests).
 EXPORTED = ("dion2_options_init", "dion2_step", "dion2_step_strided", "dion2_step_batched",
             "dion2_step_ex", "dion2_step_noalloc", "dion2_step_groups", "dion2_workspace_size",
             "dion2_workspace_size_ex", "dion2_plan_info", "dion2_plan_form",
             "dion2_release_workspaces", "dion2_status_string", "dion2_last_error",
-            "dion2_version", "dion2_profile_enable", "dion2_profile_read", "dion2_profile_reset")
+            "dion2_version", "dion2_profile_enable", "dion2_profile_read", "dion2_profile_reset",
+            "dion2_layer_options_init", "dion2_linear_forward", "dion2_linear_backward_input",
+            "dion2_linear_backward_weight", "dion2_activation_backward", "dion2_layernorm_forward",
+            "dion2_layernorm_backward", "dion2_linear_workspace_size", "dion2_layernorm_workspace_size")
 
 PHASES = ("momentum", "select", "gather", "ns_gram", "ns_poly", "ns_update", "apply")
 
@@ -80,6 +87,22 @@ class Options(ctypes.Structure):
 
 
 _lib = None
+
+
+class LayerOptions(ctypes.Structure):
+    """Mirror of struct dion2_layer_options."""
+    _fields_ = [
+        ("dtype", c_int),
+        ("p_dtype", c_int),
+        ("g_dtype", c_int),
+        ("act", c_int),
+        ("accumulate", c_int),
+        ("eps", c_float),
+        ("ld_x", c_int64), ("ld_y", c_int64), ("ld_z", c_int64), ("ld_r", c_int64),
+        ("ld_dx", c_int64), ("ld_dy", c_int64), ("ld_dz", c_int64), ("ld_dr", c_int64),
+        ("workspace", c_void_p),
+        ("workspace_bytes", c_size_t),
+    ]
 
 
 class Group(ctypes.Structure):
@@ -147,6 +170,22 @@ def load(path: str = LIB_PATH):
     lib.dion2_profile_read.restype = c_int
     lib.dion2_profile_reset.argtypes = []
     lib.dion2_profile_reset.restype = None
+    lopt = POINTER(LayerOptions)
+    lib.dion2_layer_options_init.argtypes = [lopt]
+    lib.dion2_layer_options_init.restype = None
+    lib.dion2_linear_forward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, lopt, vp]
+    lib.dion2_linear_backward_input.argtypes = [vp, vp, vp, vp, i64, i64, i64, lopt, vp]
+    lib.dion2_linear_backward_weight.argtypes = [vp, vp, vp, vp, i64, i64, i64, lopt, vp]
+    lib.dion2_activation_backward.argtypes = [vp, vp, vp, i64, i64, lopt, vp]
+    lib.dion2_layernorm_forward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, lopt, vp]
+    lib.dion2_layernorm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, lopt, vp]
+    for name in ("dion2_linear_forward", "dion2_linear_backward_input", "dion2_linear_backward_weight",
+                 "dion2_activation_backward", "dion2_layernorm_forward", "dion2_layernorm_backward"):
+        getattr(lib, name).restype = c_int
+    lib.dion2_linear_workspace_size.argtypes = [i64, i64, i64, lopt]
+    lib.dion2_linear_workspace_size.restype = c_size_t
+    lib.dion2_layernorm_workspace_size.argtypes = [i64, i64, lopt]
+    lib.dion2_layernorm_workspace_size.restype = c_size_t
     _lib = lib
     return lib
 
@@ -431,6 +470,211 @@ def dion2_plan_info(rows, cols, alpha, axis=AXIS_AUTO):
     ax = c_int(0)
     _check(load().dion2_plan_info(rows, cols, alpha, axis, ctypes.byref(k), ctypes.byref(ax)))
     return int(k.value), int(ax.value)
+
+
+# ---- the layers around the step
+
+def _rows(name, t, shape, dtype, device):
+    """A matrix of activations: unit stride along a row, any distance between rows. Returns
+    (pointer, pitch); (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    step, unit = t.stride()
+    if shape[1] > 1 and unit != 1:
+        raise ValueError(f"{name} must have unit stride along its rows")
+    if shape[0] > 1:
+        if step < shape[1]:
+            raise ValueError(f"{name}'s rows must not overlap")
+    else:
+        step = 0
+    return t.data_ptr(), step
+
+
+def _whole(name, t, shape, dtypes, device):
+    """A contiguous tensor of one of the given types. Returns its pointer; None for None."""
+    if t is None:
+        return None
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _matrix(name, t):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a HIP device tensor, got {t.device}")
+    if t.dtype not in _DT:
+        raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have 2 dimensions, got {tuple(t.shape)}")
+    return t
+
+
+def _layer_options(dtype, workspace, device):
+    opt = LayerOptions()
+    opt.dtype = _DT[dtype]
+    opt.p_dtype = opt.g_dtype = DTYPE_BF16
+    opt.eps = 1e-5
+    if workspace is not None:
+        if workspace.device != device or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous tensor on {device}")
+        opt.workspace = workspace.data_ptr()
+        opt.workspace_bytes = workspace.numel() * workspace.element_size()
+    return opt
+
+
+def _one_type(what, *tensors):
+    """The common dtype code of those that are not None (bf16 without any)."""
+    kinds = {t.dtype for t in tensors if t is not None}
+    if len(kinds) > 1:
+        raise ValueError(f"{what} must have one dtype")
+    return _DT[kinds.pop()] if kinds else DTYPE_BF16
+
+
+def _layer_call(fn, device, stream, *args):
+    """The call with its tensors' device current, on the given stream or that device's current one."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream_ptr(stream, device)))
+    else:
+        _check(fn(*args, _stream_ptr(stream, device)))
+
+
+def dion2_linear_forward(Y, X, W, *, bias=None, residual=None, Z=None, act=ACT_NONE, workspace=None,
+                         stream=None):
+    """Y = act(X W^T + bias) + residual. X [tokens, cols], W [rows, cols] (contiguous), Y, residual
+    and Z [tokens, rows], all bf16 or all fp32; bias [rows], bf16 or fp32. Z, where given, gets
+    X W^T + bias, which the gradients take. Activations may have any distance between their rows;
+    residual may be Y."""
+    dt, dev = _matrix("W", W).dtype, W.device
+    rows, cols = W.shape
+    tokens = _matrix("X", X).shape[0]
+    shape = torch.Size((tokens, rows))
+    opt = _layer_options(dt, workspace, dev)
+    opt.act = act
+    opt.p_dtype = _one_type("bias", bias)
+    x, opt.ld_x = _rows("X", X, torch.Size((tokens, cols)), dt, dev)
+    y, opt.ld_y = _rows("Y", _matrix("Y", Y), shape, dt, dev)
+    z, opt.ld_z = _rows("Z", Z, shape, dt, dev)
+    r, opt.ld_r = _rows("residual", residual, shape, dt, dev)
+    _layer_call(load().dion2_linear_forward, dev, stream, y, x, _whole("W", W, W.shape, (dt,), dev),
+                _whole("bias", bias, torch.Size((rows,)), tuple(_DT), dev), r, z, tokens, rows, cols,
+                ctypes.byref(opt))
+
+
+def dion2_linear_backward_input(dX, dY, W, *, Z=None, act=ACT_NONE, workspace=None, stream=None):
+    """dX = (dY W) * act'(Z). dY [tokens, rows], W [rows, cols] (contiguous), dX and Z
+    [tokens, cols], all bf16 or all fp32. Z is the pre-activation of the layer that made X = act(Z);
+    dX may be Z."""
+    dt, dev = _matrix("W", W).dtype, W.device
+    rows, cols = W.shape
+    tokens = _matrix("dY", dY).shape[0]
+    shape = torch.Size((tokens, cols))
+    opt = _layer_options(dt, workspace, dev)
+    opt.act = act
+    dx, opt.ld_dx = _rows("dX", _matrix("dX", dX), shape, dt, dev)
+    dy, opt.ld_dy = _rows("dY", dY, torch.Size((tokens, rows)), dt, dev)
+    z, opt.ld_z = _rows("Z", Z, shape, dt, dev)
+    _layer_call(load().dion2_linear_backward_input, dev, stream, dx, dy,
+                _whole("W", W, W.shape, (dt,), dev), z, tokens, rows, cols, ctypes.byref(opt))
+
+
+def dion2_linear_backward_weight(G, dY, X, *, dbias=None, accumulate=False, workspace=None, stream=None):
+    """G = dY^T X and dbias = dY summed over tokens, or those added to what G and dbias hold
+    (accumulate). dY [tokens, rows] and X [tokens, cols] are both bf16 or both fp32; G [rows, cols]
+    (contiguous, what the step takes) and dbias [rows] are bf16 or fp32, alike. G may be None (X
+    then too)."""
+    dt, dev = _matrix("dY", dY).dtype, dY.device
+    tokens, rows = dY.shape
+    if X is None and G is not None:
+        raise ValueError("G needs X")
+    cols = _matrix("X", X).shape[1] if X is not None else 1
+    opt = _layer_options(dt, workspace, dev)
+    opt.accumulate = 1 if accumulate else 0
+    opt.g_dtype = _one_type("G and dbias", G, dbias)
+    dy, opt.ld_dy = _rows("dY", dY, dY.shape, dt, dev)
+    x, opt.ld_x = _rows("X", X, torch.Size((tokens, cols)), dt, dev)
+    _layer_call(load().dion2_linear_backward_weight, dev, stream,
+                _whole("G", G, torch.Size((rows, cols)), tuple(_DT), dev),
+                _whole("dbias", dbias, torch.Size((rows,)), tuple(_DT), dev), dy, x, tokens, rows, cols,
+                ctypes.byref(opt))
+
+
+def dion2_activation_backward(dZ, dY, Z, act, *, stream=None):
+    """dZ = dY * act'(Z), all [tokens, width] and of one type; dZ may be dY or Z."""
+    dt, dev, shape = _matrix("dY", dY).dtype, dY.device, dY.shape
+    opt = _layer_options(dt, None, dev)
+    opt.act = act
+    dz, opt.ld_dz = _rows("dZ", _matrix("dZ", dZ), shape, dt, dev)
+    dy, opt.ld_dy = _rows("dY", dY, shape, dt, dev)
+    z, opt.ld_z = _rows("Z", _matrix("Z", Z), shape, dt, dev)
+    _layer_call(load().dion2_activation_backward, dev, stream, dz, dy, z, shape[0], shape[1],
+                ctypes.byref(opt))
+
+
+def dion2_layernorm_forward(Y, X, gamma=None, beta=None, *, eps=1e-5, mean=None, rstd=None, stream=None):
+    """Y = (X - mean) * rstd * gamma + beta per row of X [tokens, cols]; Y like X, and may be X.
+    gamma and beta [cols] are bf16 or fp32, alike (None: 1 and 0). mean and rstd, fp32 [tokens], get
+    the statistics that the gradient takes."""
+    dt, dev, shape = _matrix("X", X).dtype, X.device, X.shape
+    opt = _layer_options(dt, None, dev)
+    opt.eps = eps
+    opt.p_dtype = _one_type("gamma and beta", gamma, beta)
+    x, opt.ld_x = _rows("X", X, shape, dt, dev)
+    y, opt.ld_y = _rows("Y", _matrix("Y", Y), shape, dt, dev)
+    line, stat = shape[1:], shape[:1]
+    _layer_call(load().dion2_layernorm_forward, dev, stream, y,
+                _whole("mean", mean, stat, (torch.float32,), dev),
+                _whole("rstd", rstd, stat, (torch.float32,), dev), x,
+                _whole("gamma", gamma, line, tuple(_DT), dev), _whole("beta", beta, line, tuple(_DT), dev),
+                shape[0], shape[1], ctypes.byref(opt))
+
+
+def dion2_layernorm_backward(dX, dY, X, mean, rstd, *, gamma=None, residual_grad=None, dgamma=None,
+                             dbeta=None, accumulate=False, workspace=None, stream=None):
+    """The gradients of dion2_layernorm_forward from its mean and rstd: dX (+ residual_grad, the
+    gradient that reaches X past the norm), dgamma and dbeta [cols] (bf16 or fp32, alike; added to
+    what they hold with accumulate). Any output may be None; dX may be dY, X or residual_grad."""
+    dt, dev, shape = _matrix("dY", dY).dtype, dY.device, dY.shape
+    opt = _layer_options(dt, workspace, dev)
+    opt.accumulate = 1 if accumulate else 0
+    opt.p_dtype = _one_type("gamma", gamma)
+    opt.g_dtype = _one_type("dgamma and dbeta", dgamma, dbeta)
+    dx, opt.ld_dx = _rows("dX", dX, shape, dt, dev)
+    dy, opt.ld_dy = _rows("dY", dY, shape, dt, dev)
+    x, opt.ld_x = _rows("X", _matrix("X", X), shape, dt, dev)
+    dr, opt.ld_dr = _rows("residual_grad", residual_grad, shape, dt, dev)
+    line, stat = shape[1:], shape[:1]
+    _layer_call(load().dion2_layernorm_backward, dev, stream, dx,
+                _whole("dgamma", dgamma, line, tuple(_DT), dev), _whole("dbeta", dbeta, line, tuple(_DT), dev),
+                dy, x, _whole("mean", mean, stat, (torch.float32,), dev),
+                _whole("rstd", rstd, stat, (torch.float32,), dev),
+                _whole("gamma", gamma, line, tuple(_DT), dev), dr, shape[0], shape[1], ctypes.byref(opt))
+
+
+def dion2_linear_workspace_size(tokens, rows, cols, dtype=torch.bfloat16) -> int:
+    """Workspace bytes that suffice for every linear call of these sizes (0: none needed)."""
+    opt = LayerOptions(dtype=_DT[dtype], p_dtype=DTYPE_BF16, g_dtype=DTYPE_BF16)
+    return int(load().dion2_linear_workspace_size(tokens, rows, cols, ctypes.byref(opt)))
+
+
+def dion2_layernorm_workspace_size(tokens, cols, dtype=torch.bfloat16) -> int:
+    """Workspace bytes that suffice for every norm call of these sizes."""
+    opt = LayerOptions(dtype=_DT[dtype], p_dtype=DTYPE_BF16, g_dtype=DTYPE_BF16)
+    return int(load().dion2_layernorm_workspace_size(tokens, cols, ctypes.byref(opt)))
 
 
 def dion2_release_workspaces():

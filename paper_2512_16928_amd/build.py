@@ -32,7 +32,7 @@ LIB = os.path.join(PKG, "libdion2.so")
 ARCH = "gfx950"
 
 SOURCES = ["dion2_api.hip", "k_momentum.hip", "k_select.hip", "k_gather.hip",
-           "k_gemm.hip", "k_apply.hip"]
+           "k_gemm.hip", "k_apply.hip", "layers_api.hip", "k_linear.hip", "k_norm.hip"]
 
 # -ffp-contract=off: the elementwise stages must round exactly as written
 # (fl32(M + G), fl32(mu * M), fp64 products then differences).

@@ -23,14 +23,16 @@
 
 #include "dion2.h"
 #include "dion2_device.h"
+#include "dion2_host.h"
 
 using namespace dion2;
 
 namespace {
-
 thread_local std::string g_last_error = "no error";
+}
 
-int fail(int status, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+namespace dion2 {
+
 int fail(int status, const char* fmt, ...) {
     char buf[512];
     va_list ap;
@@ -45,9 +47,11 @@ int hip_fail(hipError_t e, const char* what) {
     return fail(DION2_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-constexpr float kMuonQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
-constexpr int64_t kMaxDim = int64_t(1) << 20;
+}  // namespace dion2
 
+namespace {
+
+constexpr float kMuonQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -263,6 +267,25 @@ int ensure_device(Workspace* w, size_t bytes) {
     w->bytes = bytes;
     return DION2_OK;
 }
+
+}  // namespace
+
+namespace dion2 {
+
+int lease_workspace(hipStream_t s, size_t bytes, WorkspaceLease* out) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+    Workspace* w = workspace_for(dev, s);
+    out->lock = std::unique_lock<std::mutex>(w->use);
+    int st = ensure_device(w, bytes);
+    if (st == DION2_OK) out->dev = static_cast<char*>(w->dev);
+    return st;
+}
+
+}  // namespace dion2
+
+namespace {
 
 // -------------------------------------------------------------- profiler
 
