@@ -81,6 +81,23 @@ __device__ __forceinline__ void each_row_of_8(const f32x16& acc, int lane, F&& f
     }
 }
 
+// A finished 32 x 32 block at rows m0.., columns n0..: its entries' epilogue,
+// or, of a product cut into parts, the sums as they are, in register order (16
+// bytes a lane), for product_join.
+template <Product KIND, typename T>
+__device__ __forceinline__ void finish_block(const ProductArgs& a, int64_t m0, int64_t n0, const f32x16& acc, int lane) {
+    if (a.splits > 1) {
+        const int64_t mb = (a.M + 31) / 32, nb = (a.N + 31) / 32;
+        if (m0 >= a.M || n0 >= a.N) return;
+        float* p = a.part + ((blockIdx.y * mb + m0 / 32) * nb + n0 / 32) * 1024 + lane * 4;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            stg(p + 256 * q, make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]));
+    } else {
+        each_row_of_8(acc, lane, [&](int r, int c, float (&v)[8]) { finish8<KIND, T>(a, m0 + r, n0 + c, v); });
+    }
+}
+
 // ---------------------------------------------------- tiles of any alignment
 // 128 x 128 tiles, four waves of 64 x 64. Operands come through registers,
 // 16 bytes a load from any element boundary, with zeros past the matrix's
@@ -248,66 +265,338 @@ __global__ __launch_bounds__(kGThreads) void product_any(ProductArgs a) {
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            each_row_of_8(acc[i][j], lane, [&](int r, int c, float (&v)[8]) {
-                const int64_t m = m0 + wm + 32 * i + r, n = n0 + wn + 32 * j + c;
-                if (a.splits > 1) {
-                    if (m < a.M && n < a.N)
-                        store8(a.part + ((int64_t)blockIdx.y * a.M + m) * a.N + n, a.N - n < 8 ? (int)(a.N - n) : 8, v);
-                } else {
-                    finish8<KIND, T>(a, m, n, v);
-                }
-            });
+            finish_block<KIND, T>(a, m0 + wm + 32 * i, n0 + wn + 32 * j, acc[i][j], lane);
 }
 
-// Adds the parts of a split product in order and finishes its entries.
-template <Product KIND, typename T>
-__global__ __launch_bounds__(256) void product_join(ProductArgs a) {
-    const int64_t chunks = (a.N + 7) / 8;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.M * chunks) return;
-    const int64_t m = i / chunks, n = i % chunks * 8;
-    const int nv = a.N - n < 8 ? (int)(a.N - n) : 8;
-    float v[8] = {};
-    for (int s = 0; s < a.splits; ++s) {
-        float x[8];
-        load8(a.part + ((int64_t)s * a.M + m) * a.N + n, nv, x);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += x[j];
+// -------------------------------------------------- bf16 tiles, LDS fed directly
+// For operands whose rows start on 16-byte boundaries. K-slices go from
+// global memory straight into LDS (16 bytes a lane, a wave's 1 KB a time), S
+// slices in flight, through buffer descriptors: a lane whose chunk lies past
+// an edge asks for an offset past the descriptor's range and gets zeros.
+//
+// k-contiguous tiles are kept [row][k] in rows of 2 BK bytes, m/n-contiguous
+// ones [k][row]; 16-byte chunks are swizzled so that the fragment reads of a
+// sixteenth of a wave (and the transposing reads' 64-byte pieces of four k)
+// fall into distinct LDS banks.
+template <int BM_, int BN_, int BK_, int S_, int WM_, int WN_>
+struct Tile {
+    static constexpr int BM = BM_, BN = BN_, BK = BK_, S = S_, WM = WM_, WN = WN_;
+    static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+    static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
+    static constexpr int A_BYTES = BM * BK * 2, STAGE = (BM + BN) * BK * 2;
+    static constexpr int LOADS = STAGE / 1024 / WAVES;   // of a wave a slice
+    static constexpr int SMEM = S * STAGE;
+    static_assert(STAGE % (1024 * WAVES) == 0 && A_BYTES % (1024 * WAVES) == 0, "whole loads");
+};
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {   // at most N of this wave's loads still on their way, no LDS read
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
+}
+
+// One operand of a tile: R rows (m or n), slices of BK.
+template <int R, int BK, int WAVES, bool KMAJOR>
+struct Operand {
+    static constexpr int PITCH = KMAJOR ? BK * 2 : R * 2;      // LDS row
+    static constexpr int CPR = PITCH / 16;
+    static constexpr int RPB = 1024 / PITCH;                   // LDS rows a 1 KB block holds
+    static constexpr int Q = R * BK * 2 / 1024 / WAVES;        // blocks a wave
+    static constexpr uint32_t OUT = 0x80000000u;               // past every descriptor's range
+    __amdgpu_buffer_rsrc_t rsrc;
+    const unsigned char* base;
+    int64_t step;          // bytes a slice
+    uint32_t off[Q];       // of the lane's chunks in the wave's blocks
+    int k_lane;            // k of the lane's chunk in the wave's first block
+    int k_left;            // from the slice loaded next on
+
+    __device__ __forceinline__ static int swizzle(int row) {
+        return KMAJOR ? (row / (256 / PITCH)) % CPR : (row & 3) << 2;
     }
-    finish8<KIND, T>(a, m, n, v);
+    // p: the operand's first row of the tile and first k; rows: of them that exist
+    __device__ __forceinline__ void init(const uint16_t* p, int64_t ld, int64_t rows, int64_t k, int wave, int lane) {
+        const int lr = lane / CPR, slot = lane % CPR;
+        const int c = slot ^ swizzle(wave * RPB + lr);   // alike in all of a wave's blocks (an even number of rows apart)
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int r = (wave + q * WAVES) * RPB + lr;
+            off[q] = (KMAJOR ? r : 8 * c) < rows ? (uint32_t)(r * ld * 2) + 16 * c : OUT;
+        }
+        k_lane = KMAJOR ? 8 * c : wave * RPB + lr;
+        base = reinterpret_cast<const unsigned char*>(p);
+        step = KMAJOR ? 2 * BK : 2 * BK * ld;
+        k_left = (int)k;
+        rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, (int)0x7ffffff0, 0x00020000);
+    }
+    __device__ __forceinline__ void load(int q, unsigned char* lds, int wave) const {
+        const uint32_t v = k_lane + (KMAJOR ? 0 : q * WAVES * RPB) < k_left ? off[q] : OUT;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + (wave + q * WAVES) * 1024),
+                                                 16, v, 0, 0, 0);
+    }
+    __device__ __forceinline__ void advance() {
+        base += step;
+        k_left -= BK;
+        rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, (int)0x7ffffff0, 0x00020000);
+    }
+    // fragment of 32 rows from `row` on, k-step kk
+    __device__ __forceinline__ static bf16x8 frag(const unsigned char* lds, int row, int kk, int lane) {
+        if constexpr (KMAJOR) {
+            const int r = row + (lane & 31), c = 2 * kk + (lane >> 5);
+            return *reinterpret_cast<const bf16x8*>(lds + r * PITCH + 16 * (c ^ swizzle(r)));
+        } else {
+            typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+            const int g = lane >> 4, s = lane & 15;
+            const int k = 16 * kk + 8 * (g >> 1) + (s >> 2);
+            const int r = row + 16 * (g & 1) + 4 * (s & 3);
+            auto at = [&](int kr) { return kr * PITCH + 16 * ((r >> 3) ^ swizzle(kr)) + 2 * (r & 7); };
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds + at(k)));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds + at(k + 4)));
+            const i16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            return __builtin_bit_cast(bf16x8, v);
+        }
+    }
+};
+
+// Which tile a block takes: each of the eight dies (blocks go to them in
+// turn) gets neighbouring ones, in columns of kGroup tiles of m, so that its
+// L2 holds the operand rows its blocks share.
+constexpr int kDies = 8, kGroup = 8;
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t total, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
+    const uint32_t q = total / kDies, r = total % kDies, die = id % kDies;
+    const uint32_t at = die * q + (die < r ? die : r) + id / kDies;
+    const uint32_t strip = at / (kGroup * tn), in = at % (kGroup * tn);
+    const uint32_t h = tm - strip * kGroup < kGroup ? tm - strip * kGroup : kGroup;
+    *m = strip * kGroup + in % h;
+    *n = in / h;
 }
 
 template <Product KIND, typename T>
-hipError_t launch_kind(const ProductArgs& a, hipStream_t s) {
-    const int64_t tiles = ((a.M + kGT - 1) / kGT) * ((a.N + kGT - 1) / kGT);
-    product_any<KIND, T><<<dim3((unsigned)tiles, (unsigned)a.splits), kGThreads, 0, s>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t chunks = a.M * ((a.N + 7) / 8);
-    product_join<KIND, T><<<(unsigned)((chunks + 255) / 256), 256, 0, s>>>(a);
+__global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
+    constexpr bool AK = KIND != PROD_WEIGHT, BKM = KIND == PROD_FORWARD;
+    using OA = Operand<T::BM, T::BK, T::WAVES, AK>;
+    using OB = Operand<T::BN, T::BK, T::WAVES, BKM>;
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / T::WN * T::TM, wn = wave % T::WN * T::TN;
+    const uint32_t tm = (uint32_t)((a.M + T::BM - 1) / T::BM), tn = (uint32_t)((a.N + T::BN - 1) / T::BN);
+    uint32_t im, in;
+    tile_of(blockIdx.x, tm * tn, tm, tn, &im, &in);
+    const int64_t m0 = (int64_t)im * T::BM, n0 = (int64_t)in * T::BN;
+    const int slices = (int)((a.K + T::BK - 1) / T::BK);
+    const int s0 = (int)((int64_t)slices * blockIdx.y / a.splits), s1 = (int)((int64_t)slices * (blockIdx.y + 1) / a.splits);
+    const int64_t k0 = (int64_t)s0 * T::BK;
+    const int64_t k_end = s1 == slices ? a.K : (int64_t)s1 * T::BK;
+    OA oa;
+    OB ob;
+    oa.init(static_cast<const uint16_t*>(a.A) + (AK ? m0 * a.lda + k0 : k0 * a.lda + m0), a.lda, a.M - m0, k_end - k0, wave, lane);
+    ob.init(static_cast<const uint16_t*>(a.B) + (BKM ? n0 * a.ldb + k0 : k0 * a.ldb + n0), a.ldb, a.N - n0, k_end - k0, wave, lane);
+    auto load = [&](int q, unsigned char* st) {
+        if (q < OA::Q) oa.load(q, st, wave);
+        else ob.load(q - OA::Q, st + T::A_BYTES, wave);
+    };
+    static_assert(OA::Q + OB::Q == T::LOADS, "every load is a whole block of one operand");
+
+    f32x16 acc[T::FM][T::FN];
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+    // The k-steps run on over slice ends: a slice's last step reads the next
+    // one's first fragments, so the barrier between them stands among queued
+    // MFMAs. Once a wave holds a slice's last fragments its stage is free.
+    // Slices past the end load zeros (k_left <= 0), so that every iteration
+    // issues and awaits the same number of loads.
+    constexpr int KK = T::BK / 16, NM = T::FM * T::FN;
+    struct Frags { bf16x8 a[T::FM], b[T::FN]; } f[2];
+    auto read = [&](Frags& x, const unsigned char* st, int kk) {
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) x.a[i] = OA::frag(st, wm + 32 * i, kk, lane);
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j) x.b[j] = OB::frag(st + T::A_BYTES, wn + 32 * j, kk, lane);
+    };
+    const int n = s1 - s0;
+#pragma unroll
+    for (int p = 0; p < T::S; ++p) {
+#pragma unroll
+        for (int q = 0; q < T::LOADS; ++q) load(q, lds + p * T::STAGE);
+        oa.advance();
+        ob.advance();
+    }
+    wait_loads<(T::S - 1) * T::LOADS>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read(f[0], lds, 0);
+    for (int s = 0; s < n; ++s) {
+        unsigned char* st = lds + s % T::S * T::STAGE;
+        const unsigned char* next = lds + (s + 1) % T::S * T::STAGE;
+#pragma unroll
+        for (int kk = 0; kk < KK - 1; ++kk) {
+            read(f[(kk + 1) & 1], st, kk + 1);
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                for (int j = 0; j < T::FN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[kk & 1].b[j], f[kk & 1].a[i], acc[i][j], 0, 0, 0);
+        }
+        // the slice's last fragments are in registers, and the next slice has
+        // landed: behind the barrier that holds for all waves
+        __builtin_amdgcn_sched_barrier(0);
+        wait_loads<(T::S - 2) * T::LOADS>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        read(f[0], next, 0);
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::FN; ++j) {
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[(KK - 1) & 1].b[j], f[(KK - 1) & 1].a[i], acc[i][j], 0, 0, 0);
+                // the freed stage's loads, spread over the MFMAs: in one burst
+                // they would hold the wave in the issue queue
+#pragma unroll
+                for (int q = 0; q < T::LOADS; ++q)
+                    if (q * NM / T::LOADS == i * T::FN + j) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        load(q, st);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
+        oa.advance();
+        ob.advance();
+    }
+    wait_loads<0>();   // none may land once LDS is another block's
+
+    // A row block at a time, through one copy of the finishing code.
+#pragma unroll 1
+    for (int i = 0; i < T::FM; ++i) {
+        f32x16 row[T::FN];
+#pragma unroll
+        for (int u = 0; u < T::FM; ++u)
+            if (u == i) {
+#pragma unroll
+                for (int j = 0; j < T::FN; ++j) row[j] = acc[u][j];
+            }
+        const int64_t mb = m0 + wm + 32 * i;
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j) finish_block<KIND, uint16_t>(a, mb, n0 + wn + 32 * j, row[j], lane);
+    }
+}
+
+// Adds the parts of a split product in order and finishes its entries: one
+// wave a 32 x 32 block.
+template <Product KIND, typename T>
+__global__ __launch_bounds__(64) void product_join(ProductArgs a) {
+    const int64_t mb = (a.M + 31) / 32, nb = (a.N + 31) / 32;
+    const float* p = a.part + (int64_t)blockIdx.x * 1024 + threadIdx.x * 4;
+    f32x16 acc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+    for (int s = 0; s < a.splits; ++s, p += mb * nb * 1024)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float4 x = ldg<float4>(p + 256 * q);
+            acc[4 * q] += x.x;
+            acc[4 * q + 1] += x.y;
+            acc[4 * q + 2] += x.z;
+            acc[4 * q + 3] += x.w;
+        }
+    const int64_t m0 = blockIdx.x / nb * 32, n0 = blockIdx.x % nb * 32;
+    each_row_of_8(acc, threadIdx.x, [&](int r, int c, float (&v)[8]) { finish8<KIND, T>(a, m0 + r, n0 + c, v); });
+}
+
+typedef Tile<256, 256, 64, 2, 2, 2> BigTile;
+typedef Tile<128, 128, 64, 2, 2, 2> SmallTile;
+
+enum Form { FORM_ANY, FORM_SMALL, FORM_BIG };
+struct Plan {
+    Form form;
+    int splits;
+};
+
+// The operands can be read in whole aligned chunks of 16 bytes.
+bool whole_chunks(Product kind, const ProductArgs& a) {
+    auto aligned = [](const void* p, int64_t ld) {
+        return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && ld < (int64_t(1) << 21);
+    };
+    const bool inner = kind == PROD_FORWARD ? a.K % 8 == 0
+                       : kind == PROD_INPUT ? a.K % 8 == 0 && a.N % 8 == 0
+                                            : a.M % 8 == 0 && a.N % 8 == 0;
+    return a.bf16 && inner && aligned(a.A, a.lda) && aligned(a.B, a.ldb);
+}
+
+int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
+
+int splits_for(int64_t tiles, int64_t K) {
+    const int64_t want = tiles >= 512 ? 1 : 512 / std::max<int64_t>(tiles, 1);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({want, (K + 63) / 64 / 4, 32}));
+}
+
+Plan plan_of(Product kind, const ProductArgs& a) {
+    Plan p;
+    p.form = !whole_chunks(kind, a) ? FORM_ANY : tiles_of(a.M, a.N, 256, 256) >= 128 ? FORM_BIG : FORM_SMALL;
+    p.splits = p.form == FORM_BIG ? 1 : splits_for(tiles_of(a.M, a.N, 128, 128), a.K);
+    return p;
+}
+
+template <Product KIND, typename T>
+hipError_t launch_tiles(const ProductArgs& a, hipStream_t s) {
+    static_assert(T::SMEM <= 160 * 1024, "LDS of a CU");
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&product_tiles<KIND, T>),
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, T::SMEM);
+    if (e != hipSuccess) return e;
+    product_tiles<KIND, T><<<dim3((unsigned)tiles_of(a.M, a.N, T::BM, T::BN), (unsigned)a.splits), T::THREADS, T::SMEM, s>>>(a);
     return hipGetLastError();
+}
+
+template <Product KIND, typename T>
+hipError_t launch_kind(const ProductArgs& a, Form form, hipStream_t s) {
+    hipError_t e = hipSuccess;
+    if constexpr (std::is_same<T, uint16_t>::value) {
+        if (form == FORM_BIG) e = launch_tiles<KIND, BigTile>(a, s);
+        else if (form == FORM_SMALL) e = launch_tiles<KIND, SmallTile>(a, s);
+    }
+    if (form == FORM_ANY) {
+        product_any<KIND, T><<<dim3((unsigned)tiles_of(a.M, a.N, kGT, kGT), (unsigned)a.splits), kGThreads, 0, s>>>(a);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess || a.splits == 1) return e;
+    product_join<KIND, T><<<(unsigned)tiles_of(a.M, a.N, 32, 32), 64, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <Product KIND>
+hipError_t launch_type(const ProductArgs& a, Form form, hipStream_t s) {
+    return a.bf16 ? launch_kind<KIND, uint16_t>(a, form, s) : launch_kind<KIND, float>(a, form, s);
+}
+
+size_t part_bytes(const ProductArgs& a, int splits) {
+    return splits > 1 ? (size_t)splits * tiles_of(a.M, a.N, 32, 32) * 4096 : 0;
 }
 
 }  // namespace
 
-int product_splits(Product kind, int64_t M, int64_t N, int64_t K, int bf16) {
-    const int64_t tiles = ((M + kGT - 1) / kGT) * ((N + kGT - 1) / kGT);
-    const int64_t slices = (K + 63) / 64;
-    // two tiles a CU, but at least 256 of k a part
-    const int64_t want = tiles >= 512 ? 1 : 512 / std::max<int64_t>(tiles, 1);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({want, slices / 4, 32}));
+size_t product_workspace(Product kind, const ProductArgs& a) { return part_bytes(a, plan_of(kind, a).splits); }
+
+size_t product_workspace_most(Product kind, int64_t M, int64_t N, int64_t K, int bf16) {
+    // the most over what pointers and pitches can make of it: chunks whole or not
+    ProductArgs a{};
+    a.M = M; a.N = N; a.K = K; a.bf16 = bf16;
+    a.lda = a.ldb = 8;
+    const size_t whole = product_workspace(kind, a);
+    a.lda = 1;
+    return std::max(whole, product_workspace(kind, a));
 }
 
-hipError_t launch_product(Product kind, const ProductArgs& a, hipStream_t s) {
+hipError_t launch_product(Product kind, ProductArgs a, hipStream_t s) {
     if (a.M == 0 || a.N == 0) return hipSuccess;
-    if (a.bf16) {
-        if (kind == PROD_FORWARD) return launch_kind<PROD_FORWARD, uint16_t>(a, s);
-        if (kind == PROD_INPUT) return launch_kind<PROD_INPUT, uint16_t>(a, s);
-        return launch_kind<PROD_WEIGHT, uint16_t>(a, s);
-    }
-    if (kind == PROD_FORWARD) return launch_kind<PROD_FORWARD, float>(a, s);
-    if (kind == PROD_INPUT) return launch_kind<PROD_INPUT, float>(a, s);
-    return launch_kind<PROD_WEIGHT, float>(a, s);
+    const Plan p = plan_of(kind, a);
+    a.splits = p.splits;
+    if (kind == PROD_FORWARD) return launch_type<PROD_FORWARD>(a, p.form, s);
+    if (kind == PROD_INPUT) return launch_type<PROD_INPUT>(a, p.form, s);
+    return launch_type<PROD_WEIGHT>(a, p.form, s);
 }
 
 }  // namespace dion2

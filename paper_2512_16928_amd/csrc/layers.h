@@ -181,12 +181,13 @@ struct ProductArgs {
     int bias_bf16;
     int out_bf16;       // type of PROD_WEIGHT's out
     int accumulate;
-    float* part;        // splits > 1: [splits][M][N] partial sums
-    int splits;
+    float* part;        // partial sums: product_workspace bytes
+    int splits;         // set by launch_product
 };
-// How many parts launch_product cuts K into for these sizes.
-int product_splits(Product kind, int64_t M, int64_t N, int64_t K, int bf16);
-hipError_t launch_product(Product kind, const ProductArgs& a, hipStream_t s);
+// Bytes of workspace of this call, and the most of any call of these sizes.
+size_t product_workspace(Product kind, const ProductArgs& a);
+size_t product_workspace_most(Product kind, int64_t M, int64_t N, int64_t K, int bf16);
+hipError_t launch_product(Product kind, ProductArgs a, hipStream_t s);
 
 // -------------------------------------------------------- streaming passes
 struct ActGradArgs {

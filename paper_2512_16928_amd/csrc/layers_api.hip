@@ -158,12 +158,9 @@ int take_scratch(const dion2_layer_options& o, size_t bytes, hipStream_t s, Scra
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
-size_t part_bytes(int splits, int64_t M, int64_t N) { return splits > 1 ? align256((size_t)splits * M * N * 4) : 0; }
-
 int run_product(Product kind, ProductArgs& a, const dion2_layer_options& o, size_t more, Scratch* ws, hipStream_t s) {
     a.bf16 = o.dtype == DION2_DTYPE_BF16;
-    a.splits = product_splits(kind, a.M, a.N, a.K, a.bf16);
-    const size_t part = part_bytes(a.splits, a.M, a.N);
+    const size_t part = product_workspace(kind, a);
     int st = take_scratch(o, part + more, s, ws);
     if (st != DION2_OK) return st;
     a.part = reinterpret_cast<float*>(ws->p);
@@ -395,10 +392,10 @@ size_t dion2_linear_workspace_size(int64_t tokens, int64_t rows, int64_t cols, c
     const dion2_layer_options o = options_of(opt);
     if (check_options(o) != DION2_OK || check_sizes(tokens, rows, cols) != DION2_OK) return 0;
     const int bf16 = o.dtype == DION2_DTYPE_BF16;
-    const size_t weight = part_bytes(product_splits(PROD_WEIGHT, rows, cols, tokens, bf16), rows, cols) +
+    const size_t weight = product_workspace_most(PROD_WEIGHT, rows, cols, tokens, bf16) +
                           align256((size_t)col_sum_blocks(tokens, rows) * rows * 4);
-    return std::max({part_bytes(product_splits(PROD_FORWARD, tokens, rows, cols, bf16), tokens, rows),
-                     part_bytes(product_splits(PROD_INPUT, tokens, cols, rows, bf16), tokens, cols), weight});
+    return std::max({product_workspace_most(PROD_FORWARD, tokens, rows, cols, bf16),
+                     product_workspace_most(PROD_INPUT, tokens, cols, rows, bf16), weight});
 }
 
 size_t dion2_layernorm_workspace_size(int64_t tokens, int64_t cols, const dion2_layer_options* opt) {
