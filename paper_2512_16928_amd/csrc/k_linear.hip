@@ -20,45 +20,66 @@ typedef __attribute__((ext_vector_type(8))) short i16x8;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 // ------------------------------------------------------------- the epilogue
-// Finishes entries n .. n + 7 of row m (those that exist) from their sums.
-template <Product KIND, typename T>
-__device__ __forceinline__ void finish8(const ProductArgs& a, int64_t m, int64_t n, float (&v)[8]) {
+// with_act where the product has an activation.
+template <Product KIND, typename F>
+__device__ __forceinline__ void with_act_of(int act, F&& f) {
+    if constexpr (KIND == PROD_WEIGHT) f(ActIs<ACT_NONE>{});
+    else with_act(act, f);
+}
+
+// The epilogue's own operand, [M][N]: the residual, the pre-activation, or
+// the gradient that is added to. Null where there is none.
+template <Product KIND>
+__device__ __forceinline__ const void* epilogue_operand(const ProductArgs& a, int64_t* ld) {
+    *ld = KIND == PROD_FORWARD ? a.ldr : KIND == PROD_INPUT ? a.ldz : a.ldo;
+    return KIND == PROD_FORWARD ? a.R : KIND == PROD_INPUT ? (a.act != ACT_NONE ? a.Z : nullptr) : (a.accumulate ? a.out : nullptr);
+}
+
+// Finishes entries n .. n + nv - 1 of row m from their sums v and the
+// operand's entries x (unused where there is none). BIAS: not in the sums yet.
+template <Product KIND, int ACT, bool BIAS, typename T>
+__device__ __forceinline__ void finish8(const ProductArgs& a, int64_t m, int64_t n, int nv, float (&v)[8], const float (&x)[8]) {
     constexpr bool FINE = std::is_same<T, float>::value;
-    if (m >= a.M || n >= a.N) return;
-    const int nv = a.N - n < 8 ? (int)(a.N - n) : 8;
-    float x[8];
     if constexpr (KIND == PROD_FORWARD) {
-        if (a.bias) {
-            load8_as(a.bias, n, a.bias_bf16, nv, x);
+        if (BIAS && a.bias) {
+            float b[8];
+            load8_as(a.bias, n, a.bias_bf16, nv, b);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += x[i];
+            for (int i = 0; i < 8; ++i) v[i] += b[i];
         }
         if (a.Z) store8(static_cast<T*>(a.Z) + m * a.ldz + n, nv, v);
-        if (a.act != ACT_NONE) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = act_value<FINE>(v[i], a.act);
-        }
+        for (int i = 0; i < 8; ++i) v[i] = act_value<ACT, FINE>(v[i]);
         if (a.R) {
-            load8(static_cast<const T*>(a.R) + m * a.ldr + n, nv, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += x[i];
         }
         store8(static_cast<T*>(a.out) + m * a.ldo + n, nv, v);
     } else if constexpr (KIND == PROD_INPUT) {
-        if (a.act != ACT_NONE) {
-            load8(static_cast<const T*>(a.Z) + m * a.ldz + n, nv, x);
+        if constexpr (ACT != ACT_NONE) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= act_slope<FINE>(x[i], a.act);
+            for (int i = 0; i < 8; ++i) v[i] *= act_slope<ACT, FINE>(x[i]);
         }
         store8(static_cast<T*>(a.out) + m * a.ldo + n, nv, v);
     } else {
         if (a.accumulate) {
-            load8_as(a.out, m * a.ldo + n, a.out_bf16, nv, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += x[i];
         }
         store8_as(a.out, m * a.ldo + n, a.out_bf16, nv, v);
     }
+}
+
+// The same where the entries may lie past the edges.
+template <Product KIND, int ACT, bool BIAS, typename T>
+__device__ __forceinline__ void finish8_edge(const ProductArgs& a, int64_t m, int64_t n, float (&v)[8]) {
+    if (m >= a.M || n >= a.N) return;
+    const int nv = a.N - n < 8 ? (int)(a.N - n) : 8;
+    float x[8];
+    int64_t ld;
+    const void* p = epilogue_operand<KIND>(a, &ld);
+    if (p) load8_as(p, m * ld + n, KIND == PROD_WEIGHT ? a.out_bf16 : std::is_same<T, uint16_t>::value, nv, x);
+    finish8<KIND, ACT, BIAS, T>(a, m, n, nv, v, x);
 }
 
 // A 32 x 32 block's accumulators hold C transposed (the B fragment is the
@@ -81,21 +102,15 @@ __device__ __forceinline__ void each_row_of_8(const f32x16& acc, int lane, F&& f
     }
 }
 
-// A finished 32 x 32 block at rows m0.., columns n0..: its entries' epilogue,
-// or, of a product cut into parts, the sums as they are, in register order (16
-// bytes a lane), for product_join.
-template <Product KIND, typename T>
-__device__ __forceinline__ void finish_block(const ProductArgs& a, int64_t m0, int64_t n0, const f32x16& acc, int lane) {
-    if (a.splits > 1) {
-        const int64_t mb = (a.M + 31) / 32, nb = (a.N + 31) / 32;
-        if (m0 >= a.M || n0 >= a.N) return;
-        float* p = a.part + ((blockIdx.y * mb + m0 / 32) * nb + n0 / 32) * 1024 + lane * 4;
+// A 32 x 32 block of a product cut into parts, at rows m0.., columns n0..: its
+// sums as they are, in register order (16 bytes a lane), for product_join.
+__device__ __forceinline__ void store_part(const ProductArgs& a, int64_t m0, int64_t n0, const f32x16& acc, int lane) {
+    if (m0 >= a.M || n0 >= a.N) return;
+    const int64_t mb = (a.M + 31) / 32, nb = (a.N + 31) / 32;
+    float* p = a.part + ((blockIdx.y * mb + m0 / 32) * nb + n0 / 32) * 1024 + lane * 4;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            stg(p + 256 * q, make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]));
-    } else {
-        each_row_of_8(acc, lane, [&](int r, int c, float (&v)[8]) { finish8<KIND, T>(a, m0 + r, n0 + c, v); });
-    }
+    for (int q = 0; q < 4; ++q)
+        stg(p + 256 * q, make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]));
 }
 
 // ---------------------------------------------------- tiles of any alignment
@@ -261,11 +276,22 @@ __global__ __launch_bounds__(kGThreads) void product_any(ProductArgs a) {
             }
         }
     }
+    if (a.splits > 1) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            finish_block<KIND, T>(a, m0 + wm + 32 * i, n0 + wn + 32 * j, acc[i][j], lane);
+            for (int j = 0; j < 2; ++j) store_part(a, m0 + wm + 32 * i, n0 + wn + 32 * j, acc[i][j], lane);
+        return;
+    }
+    with_act_of<KIND>(a.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                each_row_of_8(acc[i][j], lane, [&](int r, int c, float (&v)[8]) {
+                    finish8_edge<KIND, decltype(act)::value, true, T>(a, m0 + wm + 32 * i + r, n0 + wn + 32 * j + c, v);
+                });
+    });
 }
 
 // -------------------------------------------------- bf16 tiles, LDS fed directly
@@ -285,7 +311,10 @@ struct Tile {
     static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
     static constexpr int A_BYTES = BM * BK * 2, STAGE = (BM + BN) * BK * 2;
     static constexpr int LOADS = STAGE / 1024 / WAVES;   // of a wave a slice
+    // the epilogue's staging of a wave: 32 rows of its part of the tile, padded
+    static constexpr int EPI_ROWS = 32, EPI_LD = TN + 4;
     static constexpr int SMEM = S * STAGE;
+    static_assert(WAVES * EPI_ROWS * EPI_LD * 4 <= SMEM, "the staging fits the ring");
     static_assert(STAGE % (1024 * WAVES) == 0 && A_BYTES % (1024 * WAVES) == 0, "whole loads");
 };
 
@@ -295,8 +324,16 @@ __device__ __forceinline__ void wait_loads() {   // at most N of this wave's loa
     __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
 }
 
-// One operand of a tile: R rows (m or n), slices of BK.
-template <int R, int BK, int WAVES, bool KMAJOR>
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4)); }
+
+// One operand of a tile: R rows (m or n), slices of BK. HALF 0, 1: every first,
+// second run of 64 rows of a tile of 2 R (what a wave of a 256-row tile reads
+// in its first, second half); -1: the rows as they are.
+template <int R, int BK, int WAVES, bool KMAJOR, int HALF = -1>
 struct Operand {
     static constexpr int PITCH = KMAJOR ? BK * 2 : R * 2;      // LDS row
     static constexpr int CPR = PITCH / 16;
@@ -313,6 +350,9 @@ struct Operand {
     __device__ __forceinline__ static int swizzle(int row) {
         return KMAJOR ? (row / (256 / PITCH)) % CPR : (row & 3) << 2;
     }
+    __device__ __forceinline__ static int tile_row(int r) {
+        return HALF < 0 ? r : r / 64 * 128 + HALF * 64 + r % 64;
+    }
     // p: the operand's first row of the tile and first k; rows: of them that exist
     __device__ __forceinline__ void init(const uint16_t* p, int64_t ld, int64_t rows, int64_t k, int wave, int lane) {
         const int lr = lane / CPR, slot = lane % CPR;
@@ -320,7 +360,8 @@ struct Operand {
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int r = (wave + q * WAVES) * RPB + lr;
-            off[q] = (KMAJOR ? r : 8 * c) < rows ? (uint32_t)(r * ld * 2) + 16 * c : OUT;
+            const int row = tile_row(KMAJOR ? r : 8 * c);
+            off[q] = row < rows ? (uint32_t)(KMAJOR ? row * ld * 2 + 16 * c : r * ld * 2 + 2 * row) : OUT;
         }
         k_lane = KMAJOR ? 8 * c : wave * RPB + lr;
         base = reinterpret_cast<const unsigned char*>(p);
@@ -356,6 +397,163 @@ struct Operand {
         }
     }
 };
+
+// Finishes a wave's part of a tile. 32 rows at a time go through LDS, so that
+// a row of the output leaves in whole lines (a lane takes eight columns, TN / 8
+// lanes a row) and one copy of the code serves all of them: unrolled over the
+// accumulators it would be eight times as long. Steps of 64 / (TN / 8) rows run
+// in groups of four whose operand entries are requested one group ahead.
+template <Product KIND, int ACT, typename T, bool EDGE>
+__device__ __forceinline__ void finish_tile(const ProductArgs& a, const f32x16 (&acc)[T::FM][T::FN], float* stage, int64_t m0,
+                                            int64_t n0, int lane) {
+    constexpr int LPR = T::TN / 8, RPS = 64 / LPR, STEPS = 32 / RPS;   // lanes a row, rows a step, steps of 32 rows
+    constexpr int GROUPS = T::FM * STEPS / 4;
+    static_assert(STEPS % 4 == 0 && T::FM <= 4, "groups of four steps");
+    const int lr = lane / LPR, lc = lane % LPR * 8;
+    const int64_t n = n0 + lc;
+    const int nv = EDGE ? (int)(a.N - n < 8 ? a.N - n : 8) : 8;
+    int64_t ldx;
+    const void* xp = epilogue_operand<KIND>(a, &ldx);
+    // a gradient that is added to may be fp32: read where it is used
+    const bool ahead = xp && (KIND != PROD_WEIGHT || a.out_bf16);
+    uint4 x[4], x_next[4];
+    auto fetch = [&](int g) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t m = m0 + (4 * g + u) * RPS + lr;
+            const uint16_t* p = static_cast<const uint16_t*>(xp) + m * ldx + n;
+            if constexpr (EDGE) x_next[u] = m < a.M && nv > 0 ? load_chunk(p, nv) : make_uint4(0, 0, 0, 0);
+            else x_next[u] = ldg<uint4>(p);
+        }
+    };
+    if (ahead) fetch(0);
+#pragma unroll 1
+    for (int g = 0; g < GROUPS; ++g) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = x_next[u];
+        if (ahead && g + 1 < GROUPS) fetch(g + 1);
+        if (g % (STEPS / 4) == 0) {
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i)
+                if (i == g / (STEPS / 4)) {
+#pragma unroll
+                    for (int j = 0; j < T::FN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            *reinterpret_cast<float4*>(stage + (lane & 31) * T::EPI_LD + 32 * j + 8 * q + 4 * (lane >> 5)) =
+                                make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                }
+            __builtin_amdgcn_wave_barrier();
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int row = (4 * g + u) * RPS + lr;
+            const float4* p = reinterpret_cast<const float4*>(stage + row % 32 * T::EPI_LD + lc);
+            const float4 lo = p[0], hi = p[1];
+            float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, xv[8];
+            if constexpr (EDGE) {
+                if (m0 + row >= a.M || nv <= 0) continue;
+            }
+            if (ahead || KIND != PROD_WEIGHT || !xp) unpack8(x[u], xv);
+            else load8(static_cast<const float*>(xp) + (m0 + row) * ldx + n, nv, xv);
+            finish8<KIND, ACT, false, uint16_t>(a, m0 + row, n, nv, v, xv);
+        }
+    }
+}
+
+// The sums' start: the bias, where they are not parts (a lane's columns are
+// 8 q + 4 (lane / 32) + 0 .. 3 of a block).
+template <Product KIND, typename T>
+__device__ __forceinline__ void start_sums(const ProductArgs& a, f32x16 (&acc)[T::FM][T::FN], int64_t n0, int lane) {
+    const bool bias = KIND == PROD_FORWARD && a.bias && a.splits == 1;
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+        f32x16 start;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) start[r] = 0.0f;
+        if (bias) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                int64_t n = n0 + 32 * j + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+                n = n < a.N ? n : a.N - 1;
+                start[r] = a.bias_bf16 ? bf16_bits_to_f32(ldg<uint16_t>(static_cast<const uint16_t*>(a.bias) + n))
+                                       : ldg<float>(static_cast<const float*>(a.bias) + n);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) acc[i][j] = start;
+    }
+}
+
+// The end of a wave's sums: parts as they are, else finished through LDS.
+template <Product KIND, typename T>
+__device__ __forceinline__ void finish_sums(const ProductArgs& a, const f32x16 (&acc)[T::FM][T::FN], unsigned char* lds, int64_t m0,
+                                            int64_t n0, bool whole, int wave, int lane) {
+    wait_loads<0>();   // none may land in what LDS is used for next
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (a.splits > 1) {
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::FN; ++j) store_part(a, m0 + 32 * i, n0 + 32 * j, acc[i][j], lane);
+        return;
+    }
+    float* stage = reinterpret_cast<float*>(lds) + wave * T::EPI_ROWS * T::EPI_LD;
+    with_act_of<KIND>(a.act, [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+        if (whole) finish_tile<KIND, ACT, T, false>(a, acc, stage, m0, n0, lane);
+        else finish_tile<KIND, ACT, T, true>(a, acc, stage, m0, n0, lane);
+    });
+}
+
+// The fragments of two neighbouring blocks of 32 rows (from `row` on) over a
+// whole slice of 64: frag() for every k-step. The transposing reads are one
+// piece of assembly that ends with their wait: as the compiler's own loads,
+// each would first wait for every load to LDS still on its way.
+template <typename O, int PITCH>
+__device__ __forceinline__ void read_slice(const unsigned char* lds, int row, int lane, bf16x8 (&f)[4][2], std::true_type) {
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) f[kk][i] = O::frag(lds, row + 32 * i, kk, lane);
+}
+template <typename O, int PITCH>
+__device__ __forceinline__ void read_slice(const unsigned char* lds, int row, int lane, bf16x8 (&f)[4][2], std::false_type) {
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+    const int g = lane >> 4, s = lane & 15;
+    const int k = 8 * (g >> 1) + (s >> 2), r = row + 16 * (g & 1) + 4 * (s & 3);
+    auto at = [&](int rr) {
+        return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)(lds + k * PITCH + 16 * ((rr >> 3) ^ O::swizzle(k)) + 2 * (rr & 7));
+    };
+    const uint32_t p0 = at(r), p1 = at(r + 32);
+    u32x2 x[4][2][2];   // [k-step][block][first, second four of eight k]
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:%c18\n\t"
+        "ds_read_b64_tr_b16 %2, %17\n\tds_read_b64_tr_b16 %3, %17 offset:%c18\n\t"
+        "ds_read_b64_tr_b16 %4, %16 offset:%c19\n\tds_read_b64_tr_b16 %5, %16 offset:%c20\n\t"
+        "ds_read_b64_tr_b16 %6, %17 offset:%c19\n\tds_read_b64_tr_b16 %7, %17 offset:%c20\n\t"
+        "ds_read_b64_tr_b16 %8, %16 offset:%c21\n\tds_read_b64_tr_b16 %9, %16 offset:%c22\n\t"
+        "ds_read_b64_tr_b16 %10, %17 offset:%c21\n\tds_read_b64_tr_b16 %11, %17 offset:%c22\n\t"
+        "ds_read_b64_tr_b16 %12, %16 offset:%c23\n\tds_read_b64_tr_b16 %13, %16 offset:%c24\n\t"
+        "ds_read_b64_tr_b16 %14, %17 offset:%c23\n\tds_read_b64_tr_b16 %15, %17 offset:%c24\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0][0]), "=&v"(x[0][0][1]), "=&v"(x[0][1][0]), "=&v"(x[0][1][1]), "=&v"(x[1][0][0]), "=&v"(x[1][0][1]),
+          "=&v"(x[1][1][0]), "=&v"(x[1][1][1]), "=&v"(x[2][0][0]), "=&v"(x[2][0][1]), "=&v"(x[2][1][0]), "=&v"(x[2][1][1]),
+          "=&v"(x[3][0][0]), "=&v"(x[3][0][1]), "=&v"(x[3][1][0]), "=&v"(x[3][1][1])
+        : "v"(p0), "v"(p1), "i"(4 * PITCH), "i"(16 * PITCH), "i"(20 * PITCH), "i"(32 * PITCH), "i"(36 * PITCH), "i"(48 * PITCH),
+          "i"(52 * PITCH)
+        : "memory");
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+            const u32x4 v = {x[kk][i][0][0], x[kk][i][0][1], x[kk][i][1][0], x[kk][i][1][1]};
+            f[kk][i] = __builtin_bit_cast(bf16x8, v);
+        }
+}
 
 // Which tile a block takes: each of the eight dies (blocks go to them in
 // turn) gets neighbouring ones, in columns of kGroup tiles of m, so that its
@@ -397,12 +595,7 @@ __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
     static_assert(OA::Q + OB::Q == T::LOADS, "every load is a whole block of one operand");
 
     f32x16 acc[T::FM][T::FN];
-#pragma unroll
-    for (int i = 0; i < T::FM; ++i)
-#pragma unroll
-        for (int j = 0; j < T::FN; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    start_sums<KIND, T>(a, acc, n0 + wn, lane);
 
     // The k-steps run on over slice ends: a slice's last step reads the next
     // one's first fragments, so the barrier between them stands among queued
@@ -467,22 +660,137 @@ __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
         oa.advance();
         ob.advance();
     }
-    wait_loads<0>();   // none may land once LDS is another block's
+    finish_sums<KIND, T>(a, acc, lds, m0 + wm, n0 + wn, m0 + T::BM <= a.M && n0 + T::BN <= a.N, wave, lane);
+}
 
-    // A row block at a time, through one copy of the finishing code.
-#pragma unroll 1
-    for (int i = 0; i < T::FM; ++i) {
-        f32x16 row[T::FN];
+// 256 x 256 tiles, eight waves in two groups of four, one of each group on
+// every SIMD, that take turns: while one group's MFMAs run, the other reads its
+// next fragments and requests slices, and a barrier swaps them. A wave (128 x
+// 64 of the tile) goes through a slice of 64 in four phases:
+//   P0  reads B and the first half (64 rows) of A;  requests the next slice's
+//       second half of A
+//   C0  16 MFMAs
+//   P1  reads the second half of A;  requests B and the first half of A of the
+//       slice after the next
+//   C1  16 MFMAs
+// with the second group one phase behind. All of a slice is in registers
+// shortly after its first use, so a stage is requested again early and loads
+// have five to six of a slice's eight half-phases to arrive, with two stages.
+//
+// Requests of a slice are, in a wave's order, 6 (B and A's first half), then 2.
+// Before the phase in which the first group reads either part of slice s + 1,
+// every wave has at most 8 younger loads on their way: the barriers ahead of
+// the first group's P phases follow a wait for that, in the first group's C
+// and the second group's P phases.
+struct PairTile {
+    static constexpr int BM = 256, BN = 256, BK = 64, WM = 2, WN = 4, WAVES = 8, THREADS = 512;
+    static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
+    static constexpr int HALF_A = BM / 2 * BK * 2, B_BYTES = BN * BK * 2, STAGE = 2 * HALF_A + B_BYTES;
+    static constexpr int EPI_ROWS = 32, EPI_LD = TN + 4;
+    static constexpr int SMEM = 2 * STAGE;
+    static_assert(WAVES * EPI_ROWS * EPI_LD * 4 <= SMEM, "the staging fits the ring");
+};
+
+template <Product KIND>
+__global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a) {
+    using T = PairTile;
+    constexpr bool AK = KIND != PROD_WEIGHT, BKM = KIND == PROD_FORWARD;
+    using O0 = Operand<T::BM / 2, T::BK, T::WAVES, AK, 0>;
+    using O1 = Operand<T::BM / 2, T::BK, T::WAVES, AK, 1>;
+    using OB = Operand<T::BN, T::BK, T::WAVES, BKM>;
+    static_assert(O0::Q == 2 && O1::Q == 2 && OB::Q == 4, "loads of a wave a slice: 6 and 2");
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / T::WN, wn = wave % T::WN;
+    const bool second = wave >= 4;
+    const uint32_t tm = (uint32_t)((a.M + T::BM - 1) / T::BM), tn = (uint32_t)((a.N + T::BN - 1) / T::BN);
+    uint32_t im, in;
+    tile_of(blockIdx.x, tm * tn, tm, tn, &im, &in);
+    const int64_t m0 = (int64_t)im * T::BM, n0 = (int64_t)in * T::BN;
+    const int slices = (int)((a.K + T::BK - 1) / T::BK);
+    const int s0 = (int)((int64_t)slices * blockIdx.y / a.splits), s1 = (int)((int64_t)slices * (blockIdx.y + 1) / a.splits);
+    const int64_t k0 = (int64_t)s0 * T::BK;
+    const int64_t k = (s1 == slices ? a.K : (int64_t)s1 * T::BK) - k0;
+    const uint16_t* A = static_cast<const uint16_t*>(a.A) + (AK ? m0 * a.lda + k0 : k0 * a.lda + m0);
+    const uint16_t* B = static_cast<const uint16_t*>(a.B) + (BKM ? n0 * a.ldb + k0 : k0 * a.ldb + n0);
+    O0 o0;
+    O1 o1;
+    OB ob;
+    o0.init(A, a.lda, a.M - m0, k, wave, lane);
+    o1.init(A, a.lda, a.M - m0, k, wave, lane);
+    ob.init(B, a.ldb, a.N - n0, k, wave, lane);
+    // a stage: A's first half, its second, B
+    auto request_first = [&](unsigned char* st) {
 #pragma unroll
-        for (int u = 0; u < T::FM; ++u)
-            if (u == i) {
+        for (int q = 0; q < OB::Q; ++q) ob.load(q, st + 2 * T::HALF_A, wave);
 #pragma unroll
-                for (int j = 0; j < T::FN; ++j) row[j] = acc[u][j];
-            }
-        const int64_t mb = m0 + wm + 32 * i;
+        for (int q = 0; q < O0::Q; ++q) o0.load(q, st, wave);
+        ob.advance();
+        o0.advance();
+    };
+    auto request_second = [&](unsigned char* st) {
 #pragma unroll
-        for (int j = 0; j < T::FN; ++j) finish_block<KIND, uint16_t>(a, mb, n0 + wn + 32 * j, row[j], lane);
+        for (int q = 0; q < O1::Q; ++q) o1.load(q, st + T::HALF_A, wave);
+        o1.advance();
+    };
+
+    f32x16 acc[T::FM][T::FN];
+    start_sums<KIND, T>(a, acc, n0 + wn * T::TN, lane);
+
+    request_first(lds);
+    request_second(lds);
+    request_first(lds + T::STAGE);
+    auto swap = [&] {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    bf16x8 fa[4][2], fb[4][2];
+    auto compute = [&](auto half) {
+        constexpr int h = decltype(half)::value;
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[2 * h + i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[kk][j], fa[kk][i], acc[2 * h + i][j], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!second) wait_vmcnt<8>();
+        swap();
+    };
+    auto read_a = [&](const unsigned char* half) {
+        read_slice<O0, O0::PITCH>(half, wm * 64, lane, fa, std::bool_constant<AK>{});
+    };
+    auto end_reads = [&] {
+        __builtin_amdgcn_sched_barrier(0);
+        if (second) wait_loads<8>();
+        else wait_lds();
+        swap();
+    };
+    wait_loads<8>();
+    swap();
+    if (second) swap();
+    const int n = s1 - s0;
+    for (int s = 0; s < n; ++s) {
+        unsigned char* st = lds + (s & 1) * T::STAGE;
+        unsigned char* other = lds + T::STAGE - (s & 1) * T::STAGE;
+        request_second(other);
+        if constexpr (AK) read_a(st);
+        read_slice<OB, OB::PITCH>(st + 2 * T::HALF_A, wn * T::TN, lane, fb, std::bool_constant<BKM>{});
+        if constexpr (!AK) read_a(st);
+        end_reads();
+        compute(std::integral_constant<int, 0>{});
+        request_first(st);
+        read_a(st + T::HALF_A);
+        end_reads();
+        compute(std::integral_constant<int, 1>{});
     }
+    if (!second) swap();
+    finish_sums<KIND, T>(a, acc, lds, m0 + wm * T::TM, n0 + wn * T::TN, m0 + T::BM <= a.M && n0 + T::BN <= a.N, wave, lane);
 }
 
 // Adds the parts of a split product in order and finishes its entries: one
@@ -504,10 +812,13 @@ __global__ __launch_bounds__(64) void product_join(ProductArgs a) {
             acc[4 * q + 3] += x.w;
         }
     const int64_t m0 = blockIdx.x / nb * 32, n0 = blockIdx.x % nb * 32;
-    each_row_of_8(acc, threadIdx.x, [&](int r, int c, float (&v)[8]) { finish8<KIND, T>(a, m0 + r, n0 + c, v); });
+    with_act_of<KIND>(a.act, [&](auto act) {
+        each_row_of_8(acc, threadIdx.x, [&](int r, int c, float (&v)[8]) {
+            finish8_edge<KIND, decltype(act)::value, true, T>(a, m0 + r, n0 + c, v);
+        });
+    });
 }
 
-typedef Tile<256, 256, 64, 2, 2, 2> BigTile;
 typedef Tile<128, 128, 64, 2, 2, 2> SmallTile;
 
 enum Form { FORM_ANY, FORM_SMALL, FORM_BIG };
@@ -541,13 +852,12 @@ Plan plan_of(Product kind, const ProductArgs& a) {
     return p;
 }
 
-template <Product KIND, typename T>
-hipError_t launch_tiles(const ProductArgs& a, hipStream_t s) {
+template <typename T, typename F>
+hipError_t launch_tiles(F kernel, const ProductArgs& a, hipStream_t s) {
     static_assert(T::SMEM <= 160 * 1024, "LDS of a CU");
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&product_tiles<KIND, T>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, T::SMEM);
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, T::SMEM);
     if (e != hipSuccess) return e;
-    product_tiles<KIND, T><<<dim3((unsigned)tiles_of(a.M, a.N, T::BM, T::BN), (unsigned)a.splits), T::THREADS, T::SMEM, s>>>(a);
+    kernel<<<dim3((unsigned)tiles_of(a.M, a.N, T::BM, T::BN), (unsigned)a.splits), T::THREADS, T::SMEM, s>>>(a);
     return hipGetLastError();
 }
 
@@ -555,8 +865,8 @@ template <Product KIND, typename T>
 hipError_t launch_kind(const ProductArgs& a, Form form, hipStream_t s) {
     hipError_t e = hipSuccess;
     if constexpr (std::is_same<T, uint16_t>::value) {
-        if (form == FORM_BIG) e = launch_tiles<KIND, BigTile>(a, s);
-        else if (form == FORM_SMALL) e = launch_tiles<KIND, SmallTile>(a, s);
+        if (form == FORM_BIG) e = launch_tiles<PairTile>(&product_pairs<KIND>, a, s);
+        else if (form == FORM_SMALL) e = launch_tiles<SmallTile>(&product_tiles<KIND, SmallTile>, a, s);
     }
     if (form == FORM_ANY) {
         product_any<KIND, T><<<dim3((unsigned)tiles_of(a.M, a.N, kGT, kGT), (unsigned)a.splits), kGThreads, 0, s>>>(a);

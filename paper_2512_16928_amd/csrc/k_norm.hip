@@ -210,7 +210,7 @@ hipError_t join(const float* part, int64_t blocks, int64_t step, int64_t width, 
     return hipGetLastError();
 }
 
-template <typename T>
+template <int ACT, typename T>
 __global__ __launch_bounds__(kThreads) void act_grad(ActGradArgs a) {
     constexpr bool FINE = std::is_same<T, float>::value;
     const int64_t chunks = (a.width + 7) / 8, total = a.tokens * chunks;
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kThreads) void act_grad(ActGradArgs a) {
         load8(static_cast<const T*>(a.dY) + t * a.ldy + c, k, dy);
         load8(static_cast<const T*>(a.Z) + t * a.ldz + c, k, z);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dy[j] *= act_slope<FINE>(z[j], a.act);
+        for (int j = 0; j < 8; ++j) dy[j] *= act_slope<ACT, FINE>(z[j]);
         store8(static_cast<T*>(a.dZ) + t * a.ldo + c, k, dy);
     }
 }
@@ -249,8 +249,11 @@ hipError_t launch_act_grad(const ActGradArgs& a, hipStream_t s) {
     if (a.tokens == 0) return hipSuccess;
     const int64_t chunks = a.tokens * ((a.width + 7) / 8);
     const unsigned grid = (unsigned)std::min<int64_t>((chunks + kThreads - 1) / kThreads, 8192);
-    if (a.bf16) act_grad<uint16_t><<<grid, kThreads, 0, s>>>(a);
-    else act_grad<float><<<grid, kThreads, 0, s>>>(a);
+    auto launch = [&](auto act) {
+        if (a.bf16) act_grad<decltype(act)::value, uint16_t><<<grid, kThreads, 0, s>>>(a);
+        else act_grad<decltype(act)::value, float><<<grid, kThreads, 0, s>>>(a);
+    };
+    with_act(a.act, launch);
     return hipGetLastError();
 }
 

@@ -60,53 +60,65 @@ __device__ __forceinline__ float logistic(float x) {
 }
 
 // act(z). A NaN stays a NaN.
-template <bool FINE>
-__device__ __forceinline__ float act_value(float z, int act) {
+template <int ACT, bool FINE>
+__device__ __forceinline__ float act_value(float z) {
     float e;
-    switch (act) {
-        case ACT_RELU: return z < 0.0f ? 0.0f : z;
-        case ACT_GELU: return z * normal_cdf<FINE>(z, &e);
-        case ACT_GELU_TANH:   // z (1 + tanh v) / 2 = z logistic(2 v), v = sqrt(2 / pi) (z + 0.044715 z^3)
-            return z * logistic<FINE>(z * __builtin_fmaf(0.07135482f, z * z, 1.59576912f));
-        case ACT_SILU: return z * logistic<FINE>(z);
-        default: return z;
-    }
+    if constexpr (ACT == ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if constexpr (ACT == ACT_GELU) return z * normal_cdf<FINE>(z, &e);
+    // z (1 + tanh v) / 2 = z logistic(2 v), v = sqrt(2 / pi) (z + 0.044715 z^3)
+    if constexpr (ACT == ACT_GELU_TANH) return z * logistic<FINE>(z * __builtin_fmaf(0.07135482f, z * z, 1.59576912f));
+    if constexpr (ACT == ACT_SILU) return z * logistic<FINE>(z);
+    return z;
 }
 
 // act'(z); for ReLU 0 at 0.
-template <bool FINE>
-__device__ __forceinline__ float act_slope(float z, int act) {
-    float e;
+template <int ACT, bool FINE>
+__device__ __forceinline__ float act_slope(float z) {
+    if constexpr (ACT == ACT_RELU) return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
+    if constexpr (ACT == ACT_GELU) {
+        float e;
+        const float c = normal_cdf<FINE>(z, &e);
+        return __builtin_fmaf(z * 0.39894228f, e, c);
+    }
+    if constexpr (ACT == ACT_GELU_TANH) {
+        const float s = logistic<FINE>(z * __builtin_fmaf(0.07135482f, z * z, 1.59576912f));
+        return __builtin_fmaf(z * s * (1.0f - s), __builtin_fmaf(0.21406445f, z * z, 1.59576912f), s);
+    }
+    if constexpr (ACT == ACT_SILU) {
+        const float s = logistic<FINE>(z);
+        return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
+    }
+    return 1.0f;
+}
+
+// f with the activation as a compile-time constant: one uniform branch for
+// all the entries that f handles.
+template <int A> struct ActIs { static constexpr int value = A; };
+template <typename F>
+__host__ __device__ __forceinline__ void with_act(int act, F&& f) {
     switch (act) {
-        case ACT_RELU: return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
-        case ACT_GELU: {
-            const float c = normal_cdf<FINE>(z, &e);
-            return __builtin_fmaf(z * 0.39894228f, e, c);
-        }
-        case ACT_GELU_TANH: {
-            const float s = logistic<FINE>(z * __builtin_fmaf(0.07135482f, z * z, 1.59576912f));
-            return __builtin_fmaf(z * s * (1.0f - s), __builtin_fmaf(0.21406445f, z * z, 1.59576912f), s);
-        }
-        case ACT_SILU: {
-            const float s = logistic<FINE>(z);
-            return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
-        }
-        default: return 1.0f;
+        case ACT_RELU: f(ActIs<ACT_RELU>{}); break;
+        case ACT_GELU: f(ActIs<ACT_GELU>{}); break;
+        case ACT_GELU_TANH: f(ActIs<ACT_GELU_TANH>{}); break;
+        case ACT_SILU: f(ActIs<ACT_SILU>{}); break;
+        default: f(ActIs<ACT_NONE>{}); break;
     }
 }
 
 // ------------------------------------------------- eight consecutive entries
 // of a row, of which the first n exist (the others read as zero and are not
 // written); any alignment of whole elements.
+__device__ __forceinline__ void unpack8(const uint4& x, float (&v)[8]) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
 __device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) {
     if (n >= 8) {
-        const uint4 x = ldg<uint4>(p);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = bf16_bits_to_f32(w[i] & 0xffffu);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
+        unpack8(ldg<uint4>(p), v);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < n ? bf16_bits_to_f32(ldg<uint16_t>(p + i)) : 0.0f;
