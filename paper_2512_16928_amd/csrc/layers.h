@@ -251,9 +251,10 @@ struct NormGradArgs {
     int64_t lddy, ldx, lddr, lddx, tokens, cols;
     int bf16, p_bf16, g_bf16, accumulate;
     float* part;        // [blocks][2][cols], where dgamma or dbeta is set
-    int64_t blocks;     // norm_grad_blocks(tokens, cols)
+    int64_t blocks;     // norm_grad_blocks(...)
+    int64_t run;        // rows a block; set by launch_norm_grad
 };
-int64_t norm_grad_blocks(int64_t tokens, int64_t cols);
-hipError_t launch_norm_grad(const NormGradArgs& a, hipStream_t s);
+int64_t norm_grad_blocks(int64_t tokens, int64_t cols, int bf16);
+hipError_t launch_norm_grad(NormGradArgs a, hipStream_t s);
 
 }  // namespace dion2

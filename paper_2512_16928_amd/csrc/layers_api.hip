@@ -325,7 +325,7 @@ int layernorm_backward(void* dX, void* dgamma, void* dbeta, const void* dY, cons
     a.tokens = tokens; a.cols = cols;
     a.bf16 = o.dtype == DION2_DTYPE_BF16; a.p_bf16 = o.p_dtype == DION2_DTYPE_BF16;
     a.g_bf16 = o.g_dtype == DION2_DTYPE_BF16; a.accumulate = o.accumulate != 0;
-    a.blocks = norm_grad_blocks(tokens, cols);
+    a.blocks = norm_grad_blocks(tokens, cols, a.bf16);
     Scratch ws;
     st = take_scratch(o, dgamma || dbeta ? align256((size_t)a.blocks * 2 * cols * 4) : 0, s, &ws);
     if (st != DION2_OK) return st;
@@ -401,7 +401,7 @@ size_t dion2_linear_workspace_size(int64_t tokens, int64_t rows, int64_t cols, c
 size_t dion2_layernorm_workspace_size(int64_t tokens, int64_t cols, const dion2_layer_options* opt) {
     const dion2_layer_options o = options_of(opt);
     if (check_options(o) != DION2_OK || check_sizes(tokens, 1, cols) != DION2_OK) return 0;
-    return align256((size_t)norm_grad_blocks(tokens, cols) * 2 * cols * 4);
+    return align256((size_t)norm_grad_blocks(tokens, cols, o.dtype == DION2_DTYPE_BF16) * 2 * cols * 4);
 }
 
 }  // extern "C"
