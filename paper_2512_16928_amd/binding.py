@@ -546,11 +546,17 @@ def _one_type(what, *tensors):
 
 def _layer_call(fn, device, stream, *args):
     """The call with its tensors' device current, on the given stream or that device's current one."""
+    if stream is None:
+        ptr = torch._C._cuda_getCurrentRawStream(device.index)   # current_stream() without the object
+    else:
+        ptr = stream.cuda_stream
     if device.index != torch.cuda.current_device():
         with torch.cuda.device(device):
-            _check(fn(*args, _stream_ptr(stream, device)))
+            status = fn(*args, ptr)
     else:
-        _check(fn(*args, _stream_ptr(stream, device)))
+        status = fn(*args, ptr)
+    if status != DION2_OK:
+        _check(status)
 
 
 def dion2_linear_forward(Y, X, W, *, bias=None, residual=None, Z=None, act=ACT_NONE, workspace=None,

@@ -114,21 +114,21 @@ __device__ __forceinline__ void store_part(const ProductArgs& a, int64_t m0, int
 }
 
 // ---------------------------------------------------- tiles of any alignment
-// 128 x 128 tiles, four waves of 64 x 64. Operands come through registers,
-// 16 bytes a load from any element boundary, with zeros past the matrix's
-// edges, one slice ahead of the MFMAs, into one of two LDS buffers.
+// 128 x 128 tiles, four waves of 64 x 64, or 64 x 64 tiles, four waves of 32 x
+// 32, with slices twice as deep, in launches of few tiles. Operands come
+// through registers, 16 bytes a load from any element boundary, with zeros past
+// the matrix's edges, one slice ahead of the MFMAs, into one of two LDS buffers.
 //
-// bf16: slices of 32. k-contiguous operands are kept [row][k], m/n-contiguous
-// ones [k][row] and read with the transposing LDS read; both with their
-// 16-byte chunks swizzled against bank conflicts. fp32: slices of 16, always
-// kept [k][row] (a fragment of v_mfma_f32_32x32x2_f32 is one float of 32
-// consecutive rows), rows padded by 16 bytes.
-constexpr int kGT = 128;
+// bf16: slices of 32 (64). k-contiguous operands are kept [row][k],
+// m/n-contiguous ones [k][row] and read with the transposing LDS read; both
+// with their 16-byte chunks swizzled against bank conflicts. fp32: slices of 16
+// (32), always kept [k][row] (a fragment of v_mfma_f32_32x32x2_f32 is one float
+// of 32 consecutive rows), rows padded by 16 bytes.
 constexpr int kGThreads = 256;
 
-template <typename T> struct GSlice;
-template <> struct GSlice<uint16_t> { static constexpr int K = 32, BYTES = kGT * 64; };
-template <> struct GSlice<float> { static constexpr int K = 16, LD = kGT + 4, BYTES = 16 * LD * 4; };
+template <typename T, int GT> struct GSlice;
+template <int GT> struct GSlice<uint16_t, GT> { static constexpr int K = 4096 / GT, BYTES = GT * K * 2; };
+template <int GT> struct GSlice<float, GT> { static constexpr int K = 2048 / GT, LD = GT + 4, BYTES = K * LD * 4; };
 
 __device__ __forceinline__ uint4 load_chunk(const uint16_t* p, int n) {
     if (n >= 8) return ldg<uint4>(p);
@@ -148,12 +148,15 @@ __device__ __forceinline__ uint4 load_chunk(const float* p, int n) {
 }
 
 // One operand's part of a slice: two 16-byte chunks a thread.
-template <typename T, bool KMAJOR>
+template <typename T, int GT, bool KMAJOR>
 struct GOperand {
     static constexpr int E = 16 / sizeof(T);        // entries a chunk
-    static constexpr int SK = GSlice<T>::K;
-    static constexpr int CPR = (KMAJOR ? SK : kGT) / E;   // chunks a stored row
+    static constexpr int SK = GSlice<T, GT>::K;
+    static constexpr int CPR = (KMAJOR ? SK : GT) / E;   // chunks a stored row
+    static constexpr int PITCH = CPR * 16;               // bytes of a bf16 one
     uint4 reg[2];
+
+    __device__ __forceinline__ static int swizzle(int row) { return KMAJOR ? (row / (PITCH < 256 ? 256 / PITCH : 1)) % CPR : (row & 3) << (GT == 128 ? 2 : 1); }
 
     // row0: the tile's first row (m or n); rows, K: the operand's extents
     __device__ __forceinline__ void load(const T* p, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t K, int tid) {
@@ -173,16 +176,15 @@ struct GOperand {
             const int i = tid + q * kGThreads;
             const int r = i / CPR, c = i % CPR;
             if constexpr (sizeof(T) == 2) {
-                const int off = KMAJOR ? r * 64 + 16 * (c ^ ((r / 4) % 4)) : r * 256 + 16 * (c ^ ((r & 3) << 2));
-                *reinterpret_cast<uint4*>(lds + off) = reg[q];
+                *reinterpret_cast<uint4*>(lds + r * PITCH + 16 * (c ^ swizzle(r))) = reg[q];
             } else {
                 float* f = reinterpret_cast<float*>(lds);
                 if constexpr (KMAJOR) {
                     const uint32_t w[4] = {reg[q].x, reg[q].y, reg[q].z, reg[q].w};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) f[(4 * c + j) * GSlice<float>::LD + r] = __uint_as_float(w[j]);
+                    for (int j = 0; j < 4; ++j) f[(4 * c + j) * GSlice<float, GT>::LD + r] = __uint_as_float(w[j]);
                 } else {
-                    *reinterpret_cast<uint4*>(f + r * GSlice<float>::LD + 4 * c) = reg[q];
+                    *reinterpret_cast<uint4*>(f + r * GSlice<float, GT>::LD + 4 * c) = reg[q];
                 }
             }
         }
@@ -190,11 +192,11 @@ struct GOperand {
 };
 
 // Fragment of 32 rows from `row` on, k-step kk, of a bf16 operand.
-template <bool KMAJOR>
+template <typename O, bool KMAJOR>
 __device__ __forceinline__ bf16x8 g_frag(const unsigned char* lds, int row, int kk, int lane) {
     if constexpr (KMAJOR) {
         const int r = row + (lane & 31), c = 2 * kk + (lane >> 5);
-        return *reinterpret_cast<const bf16x8*>(lds + r * 64 + 16 * (c ^ ((r / 4) % 4)));
+        return *reinterpret_cast<const bf16x8*>(lds + r * O::PITCH + 16 * (c ^ O::swizzle(r)));
     } else {
         // a lane of a 16-lane group receives element (i mod 4) of the 8 bytes
         // addressed by source lane 4 e + i / 4, e = 0 .. 3
@@ -202,7 +204,7 @@ __device__ __forceinline__ bf16x8 g_frag(const unsigned char* lds, int row, int 
         const int g = lane >> 4, s = lane & 15;
         const int k = 16 * kk + 8 * (g >> 1) + (s >> 2);
         const int r = row + 16 * (g & 1) + 4 * (s & 3);
-        auto at = [&](int kr) { return kr * 256 + 16 * ((r >> 3) ^ ((kr & 3) << 2)) + 2 * (r & 7); };
+        auto at = [&](int kr) { return kr * O::PITCH + 16 * ((r >> 3) ^ O::swizzle(kr)) + 2 * (r & 7); };
         const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds + at(k)));
         const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds + at(k + 4)));
         const i16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -210,26 +212,28 @@ __device__ __forceinline__ bf16x8 g_frag(const unsigned char* lds, int row, int 
     }
 }
 
-template <Product KIND, typename T>
+template <Product KIND, typename T, int GT>
 __global__ __launch_bounds__(kGThreads) void product_any(ProductArgs a) {
     constexpr bool AK = KIND != PROD_WEIGHT, BKM = KIND == PROD_FORWARD;
-    constexpr int SK = GSlice<T>::K, SB = GSlice<T>::BYTES;
+    constexpr int SK = GSlice<T, GT>::K, SB = GSlice<T, GT>::BYTES, F = GT / 64;   // F x F blocks a wave
     __shared__ __align__(16) unsigned char lds[2][2][SB];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-    const int64_t tiles_n = (a.N + kGT - 1) / kGT;
-    const int64_t m0 = blockIdx.x / tiles_n * kGT, n0 = blockIdx.x % tiles_n * kGT;
+    const int wm = (wave >> 1) * 32 * F, wn = (wave & 1) * 32 * F;
+    const int64_t tiles_n = (a.N + GT - 1) / GT;
+    const int64_t m0 = blockIdx.x / tiles_n * GT, n0 = blockIdx.x % tiles_n * GT;
     const int64_t slices = (a.K + SK - 1) / SK;
     const int64_t s0 = slices * blockIdx.y / a.splits, s1 = slices * (blockIdx.y + 1) / a.splits;
     const T* A = static_cast<const T*>(a.A);
     const T* B = static_cast<const T*>(a.B);
-    GOperand<T, AK> ga;
-    GOperand<T, BKM> gb;
-    f32x16 acc[2][2];
+    using GA = GOperand<T, GT, AK>;
+    using GB = GOperand<T, GT, BKM>;
+    GA ga;
+    GB gb;
+    f32x16 acc[F][F];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < F; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < F; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
     if (s0 < s1) {
@@ -249,16 +253,16 @@ __global__ __launch_bounds__(kGThreads) void product_any(ProductArgs a) {
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
             for (int kk = 0; kk < SK / 16; ++kk) {
-                bf16x8 fa[2], fb[2];
+                bf16x8 fa[F], fb[F];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    fa[i] = g_frag<AK>(la, wm + 32 * i, kk, lane);
-                    fb[i] = g_frag<BKM>(lb, wn + 32 * i, kk, lane);
+                for (int i = 0; i < F; ++i) {
+                    fa[i] = g_frag<GA, AK>(la, wm + 32 * i, kk, lane);
+                    fb[i] = g_frag<GB, BKM>(lb, wn + 32 * i, kk, lane);
                 }
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < F; ++i)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
+                    for (int j = 0; j < F; ++j)
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
             }
         } else {
@@ -266,28 +270,33 @@ __global__ __launch_bounds__(kGThreads) void product_any(ProductArgs a) {
             const float* pb = reinterpret_cast<const float*>(lb) + wn + (lane & 31);
 #pragma unroll
             for (int kk = 0; kk < SK / 2; ++kk) {
-                const int k = (2 * kk + (lane >> 5)) * GSlice<float>::LD;
-                const float fa[2] = {pa[k], pa[k + 32]}, fb[2] = {pb[k], pb[k + 32]};
+                const int k = (2 * kk + (lane >> 5)) * GSlice<float, GT>::LD;
+                float fa[F], fb[F];
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < F; ++i) {
+                    fa[i] = pa[k + 32 * i];
+                    fb[i] = pb[k + 32 * i];
+                }
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
+                for (int i = 0; i < F; ++i)
+#pragma unroll
+                    for (int j = 0; j < F; ++j)
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[j], fa[i], acc[i][j], 0, 0, 0);
             }
         }
     }
     if (a.splits > 1) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < F; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) store_part(a, m0 + wm + 32 * i, n0 + wn + 32 * j, acc[i][j], lane);
+            for (int j = 0; j < F; ++j) store_part(a, m0 + wm + 32 * i, n0 + wn + 32 * j, acc[i][j], lane);
         return;
     }
     with_act_of<KIND>(a.act, [&](auto act) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < F; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < F; ++j)
                 each_row_of_8(acc[i][j], lane, [&](int r, int c, float (&v)[8]) {
                     finish8_edge<KIND, decltype(act)::value, true, T>(a, m0 + wm + 32 * i + r, n0 + wn + 32 * j + c, v);
                 });
@@ -348,7 +357,7 @@ struct Operand {
     int k_left;            // from the slice loaded next on
 
     __device__ __forceinline__ static int swizzle(int row) {
-        return KMAJOR ? (row / (256 / PITCH)) % CPR : (row & 3) << 2;
+        return KMAJOR ? (row / (PITCH < 256 ? 256 / PITCH : 1)) % CPR : (row & 3) << 2;
     }
     __device__ __forceinline__ static int tile_row(int r) {
         return HALF < 0 ? r : r / 64 * 128 + HALF * 64 + r % 64;
@@ -793,6 +802,66 @@ __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a
     finish_sums<KIND, T>(a, acc, lds, m0 + wm * T::TM, n0 + wn * T::TN, m0 + T::BM <= a.M && n0 + T::BN <= a.N, wave, lane);
 }
 
+// ----------------------------------------------------------- few tokens
+// Y for at most 32 tokens (an answering model's steps): W's rows are the work,
+// read once, straight into MFMA fragments (16 x 16 x 32: a lane has 8
+// consecutive k of one of 16 rows, so an instruction reads 64-byte pieces); a
+// block's waves share 16 rows, each a run of k, and add up in LDS.
+template <int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void product_few(ProductArgs a) {
+    constexpr int U = NT == 1 ? 8 : 4;    // k-steps whose loads are on their way together
+    typedef __attribute__((ext_vector_type(4))) float f32x4;
+    __shared__ __align__(16) float part[WAVES][NT][16][20];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int kl = 8 * (lane >> 4);
+    // rows past the edges read the last one; what they give is not stored
+    const int64_t n = n0 + (lane & 15);
+    const uint16_t* w = static_cast<const uint16_t*>(a.B) + (n < a.N ? n : a.N - 1) * a.ldb + kl;
+    const uint16_t* x[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int64_t m = 16 * t + (lane & 15);
+        x[t] = static_cast<const uint16_t*>(a.A) + (m < a.M ? m : a.M - 1) * a.lda + kl;
+    }
+    f32x4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int K = (int)a.K, steps = (K + 31) / 32;
+    const int s1 = steps * (wave + 1) / WAVES;
+    for (int s = steps * wave / WAVES; s < s1; s += U) {
+        uint4 fw[U], fx[U][NT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool in = s + u < s1 && 32 * (s + u) + kl < K;
+            fw[u] = in ? ldg<uint4>(w + 32 * (s + u)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) fx[u][t] = in ? ldg<uint4>(x[t] + 32 * (s + u)) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[u]),
+                                                                 __builtin_bit_cast(bf16x8, fx[u][t]), acc[t], 0, 0, 0);
+    }
+    // lane l has rows 4 (l / 16) + 0 .. 3 of token l mod 16
+#pragma unroll
+    for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(&part[wave][t][lane & 15][4 * (lane >> 4)]) = acc[t];
+    __syncthreads();
+    const int id = threadIdx.x;
+    if (id >= 32 * NT) return;
+    const int t = id / 32, tok = id / 2 % 16, c = 8 * (id & 1);
+    float v[8] = {};
+#pragma unroll
+    for (int g = 0; g < WAVES; ++g)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += part[g][t][tok][c + j];
+    with_act(a.act, [&](auto act) {
+        finish8_edge<PROD_FORWARD, decltype(act)::value, true, uint16_t>(a, 16 * t + tok, n0 + c, v);
+    });
+}
+
 // Adds the parts of a split product in order and finishes its entries: one
 // wave a 32 x 32 block.
 template <Product KIND, typename T>
@@ -821,7 +890,7 @@ __global__ __launch_bounds__(64) void product_join(ProductArgs a) {
 
 typedef Tile<128, 128, 64, 2, 2, 2> SmallTile;
 
-enum Form { FORM_ANY, FORM_SMALL, FORM_BIG };
+enum Form { FORM_ANY, FORM_ANY_64, FORM_FEW, FORM_SMALL, FORM_BIG };
 struct Plan {
     Form form;
     int splits;
@@ -840,15 +909,30 @@ bool whole_chunks(Product kind, const ProductArgs& a) {
 
 int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
 
-int splits_for(int64_t tiles, int64_t K) {
-    const int64_t want = tiles >= 512 ? 1 : 512 / std::max<int64_t>(tiles, 1);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({want, (K + 63) / 64 / 4, 32}));
+// Parts of K that bring a launch to about `blocks` blocks, each of `least` of
+// K or more.
+int splits_for(int64_t tiles, int64_t K, int64_t blocks, int64_t least) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>({blocks / std::max<int64_t>(tiles, 1), K / least, 32}));
 }
 
 Plan plan_of(Product kind, const ProductArgs& a) {
-    Plan p;
-    p.form = !whole_chunks(kind, a) ? FORM_ANY : tiles_of(a.M, a.N, 256, 256) >= 128 ? FORM_BIG : FORM_SMALL;
-    p.splits = p.form == FORM_BIG ? 1 : splits_for(tiles_of(a.M, a.N, 128, 128), a.K);
+    Plan p{FORM_ANY, 1};
+    const int64_t tiles = tiles_of(a.M, a.N, 128, 128);
+    if (!whole_chunks(kind, a)) {
+        if (tiles < 128) {
+            p.form = FORM_ANY_64;
+            p.splits = splits_for(tiles_of(a.M, a.N, 64, 64), a.K, 512, 128);
+        } else {
+            p.splits = splits_for(tiles, a.K, 512, 256);
+        }
+    } else if (kind == PROD_FORWARD && a.M <= 32) {
+        p.form = FORM_FEW;
+    } else if (tiles_of(a.M, a.N, 256, 256) >= 128) {
+        p.form = FORM_BIG;
+    } else {
+        p.form = FORM_SMALL;
+        p.splits = splits_for(tiles, a.K, 512, 256);
+    }
     return p;
 }
 
@@ -861,17 +945,31 @@ hipError_t launch_tiles(F kernel, const ProductArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <Product KIND, typename T, int GT>
+hipError_t launch_any(const ProductArgs& a, hipStream_t s) {
+    product_any<KIND, T, GT><<<dim3((unsigned)tiles_of(a.M, a.N, GT, GT), (unsigned)a.splits), kGThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_few(const ProductArgs& a, hipStream_t s) {
+    const unsigned blocks = (unsigned)((a.N + 15) / 16);
+    // sixteen waves where a run of k still is eight loads of each
+    if (a.M > 16) product_few<2, 8><<<blocks, 512, 0, s>>>(a);
+    else if (a.K >= 16 * 8 * 32) product_few<1, 16><<<blocks, 1024, 0, s>>>(a);
+    else product_few<1, 8><<<blocks, 512, 0, s>>>(a);
+    return hipGetLastError();
+}
+
 template <Product KIND, typename T>
 hipError_t launch_kind(const ProductArgs& a, Form form, hipStream_t s) {
     hipError_t e = hipSuccess;
     if constexpr (std::is_same<T, uint16_t>::value) {
         if (form == FORM_BIG) e = launch_tiles<PairTile>(&product_pairs<KIND>, a, s);
         else if (form == FORM_SMALL) e = launch_tiles<SmallTile>(&product_tiles<KIND, SmallTile>, a, s);
+        else if (form == FORM_FEW) return launch_few(a, s);
     }
-    if (form == FORM_ANY) {
-        product_any<KIND, T><<<dim3((unsigned)tiles_of(a.M, a.N, kGT, kGT), (unsigned)a.splits), kGThreads, 0, s>>>(a);
-        e = hipGetLastError();
-    }
+    if (form == FORM_ANY) e = launch_any<KIND, T, 128>(a, s);
+    else if (form == FORM_ANY_64) e = launch_any<KIND, T, 64>(a, s);
     if (e != hipSuccess || a.splits == 1) return e;
     product_join<KIND, T><<<(unsigned)tiles_of(a.M, a.N, 32, 32), 64, 0, s>>>(a);
     return hipGetLastError();

@@ -86,11 +86,12 @@ def product64(a, b):
     return a @ b, (a.shape[1] + 16) * 2.0 ** -23 * (a.abs() @ b.abs())
 
 
-# (tokens, rows, cols): one entry, single tokens, below and above a vector, tile edges, odd and large; the last three have
-# an output of 144 partly filled 256 x 256 tiles in one of the three products
+# (tokens, rows, cols): one entry, single tokens, below and above a vector, tile edges, odd and large, an
+# output of 144 partly filled 256 x 256 tiles in each of the three products, and as many tokens as fill one or two of 16
 SIZES = [(1, 1, 1), (1, 96, 64), (1, 257, 1000), (2, 33, 7), (3, 8, 130), (5, 1000, 264), (16, 300, 520), (17, 64, 64),
          (31, 7, 33), (64, 128, 128), (127, 129, 130), (128, 256, 512), (129, 100, 8), (300, 264, 257), (515, 130, 72),
-         (1024, 520, 2048), (700, 1000, 517), (2900, 2824, 200), (2900, 72, 2824), (72, 2904, 2824)]
+         (1024, 520, 2048), (700, 1000, 517), (2900, 2824, 200), (2900, 72, 2824), (72, 2904, 2824),
+         (16, 1000, 4104), (32, 520, 2048), (33, 264, 264)]
 ACTS = sorted(ACTIVATIONS)
 
 
