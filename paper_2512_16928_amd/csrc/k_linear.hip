@@ -357,7 +357,7 @@ struct Operand {
     int k_left;            // from the slice loaded next on
 
     __device__ __forceinline__ static int swizzle(int row) {
-        return KMAJOR ? (row / (PITCH < 256 ? 256 / PITCH : 1)) % CPR : (row & 3) << 2;
+        return KMAJOR ? (row / (PITCH < 256 ? 256 / PITCH : 1)) % CPR : (row & 3) << (PITCH < 256 ? 1 : 2);
     }
     __device__ __forceinline__ static int tile_row(int r) {
         return HALF < 0 ? r : r / 64 * 128 + HALF * 64 + r % 64;
@@ -388,36 +388,18 @@ struct Operand {
         k_left -= BK;
         rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, (int)0x7ffffff0, 0x00020000);
     }
-    // fragment of 32 rows from `row` on, k-step kk
-    __device__ __forceinline__ static bf16x8 frag(const unsigned char* lds, int row, int kk, int lane) {
-        if constexpr (KMAJOR) {
-            const int r = row + (lane & 31), c = 2 * kk + (lane >> 5);
-            return *reinterpret_cast<const bf16x8*>(lds + r * PITCH + 16 * (c ^ swizzle(r)));
-        } else {
-            typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-            const int g = lane >> 4, s = lane & 15;
-            const int k = 16 * kk + 8 * (g >> 1) + (s >> 2);
-            const int r = row + 16 * (g & 1) + 4 * (s & 3);
-            auto at = [&](int kr) { return kr * PITCH + 16 * ((r >> 3) ^ swizzle(kr)) + 2 * (r & 7); };
-            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds + at(k)));
-            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds + at(k + 4)));
-            const i16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            return __builtin_bit_cast(bf16x8, v);
-        }
-    }
 };
 
 // Finishes a wave's part of a tile. 32 rows at a time go through LDS, so that
 // a row of the output leaves in whole lines (a lane takes eight columns, TN / 8
 // lanes a row) and one copy of the code serves all of them: unrolled over the
 // accumulators it would be eight times as long. Steps of 64 / (TN / 8) rows run
-// in groups of four whose operand entries are requested one group ahead.
+// in groups (of four) whose operand entries are requested one group ahead.
 template <Product KIND, int ACT, typename T, bool EDGE>
 __device__ __forceinline__ void finish_tile(const ProductArgs& a, const f32x16 (&acc)[T::FM][T::FN], float* stage, int64_t m0,
                                             int64_t n0, int lane) {
     constexpr int LPR = T::TN / 8, RPS = 64 / LPR, STEPS = 32 / RPS;   // lanes a row, rows a step, steps of 32 rows
-    constexpr int GROUPS = T::FM * STEPS / 4;
-    static_assert(STEPS % 4 == 0 && T::FM <= 4, "groups of four steps");
+    constexpr int G = STEPS < 4 ? STEPS : 4, GROUPS = T::FM * STEPS / G;   // steps a group
     const int lr = lane / LPR, lc = lane % LPR * 8;
     const int64_t n = n0 + lc;
     const int nv = EDGE ? (int)(a.N - n < 8 ? a.N - n : 8) : 8;
@@ -425,11 +407,11 @@ __device__ __forceinline__ void finish_tile(const ProductArgs& a, const f32x16 (
     const void* xp = epilogue_operand<KIND>(a, &ldx);
     // a gradient that is added to may be fp32: read where it is used
     const bool ahead = xp && (KIND != PROD_WEIGHT || a.out_bf16);
-    uint4 x[4], x_next[4];
+    uint4 x[G], x_next[G];
     auto fetch = [&](int g) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t m = m0 + (4 * g + u) * RPS + lr;
+        for (int u = 0; u < G; ++u) {
+            const int64_t m = m0 + (G * g + u) * RPS + lr;
             const uint16_t* p = static_cast<const uint16_t*>(xp) + m * ldx + n;
             if constexpr (EDGE) x_next[u] = m < a.M && nv > 0 ? load_chunk(p, nv) : make_uint4(0, 0, 0, 0);
             else x_next[u] = ldg<uint4>(p);
@@ -439,13 +421,13 @@ __device__ __forceinline__ void finish_tile(const ProductArgs& a, const f32x16 (
 #pragma unroll 1
     for (int g = 0; g < GROUPS; ++g) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = x_next[u];
+        for (int u = 0; u < G; ++u) x[u] = x_next[u];
         if (ahead && g + 1 < GROUPS) fetch(g + 1);
-        if (g % (STEPS / 4) == 0) {
+        if (g % (STEPS / G) == 0) {
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int i = 0; i < T::FM; ++i)
-                if (i == g / (STEPS / 4)) {
+                if (i == g / (STEPS / G)) {
 #pragma unroll
                     for (int j = 0; j < T::FN; ++j)
 #pragma unroll
@@ -456,8 +438,8 @@ __device__ __forceinline__ void finish_tile(const ProductArgs& a, const f32x16 (
             __builtin_amdgcn_wave_barrier();
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int row = (4 * g + u) * RPS + lr;
+        for (int u = 0; u < G; ++u) {
+            const int row = (G * g + u) * RPS + lr;
             const float4* p = reinterpret_cast<const float4*>(stage + row % 32 * T::EPI_LD + lc);
             const float4 lo = p[0], hi = p[1];
             float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, xv[8];
@@ -517,26 +499,55 @@ __device__ __forceinline__ void finish_sums(const ProductArgs& a, const f32x16 (
     });
 }
 
-// The fragments of two neighbouring blocks of 32 rows (from `row` on) over a
-// whole slice of 64: frag() for every k-step. The transposing reads are one
-// piece of assembly that ends with their wait: as the compiler's own loads,
-// each would first wait for every load to LDS still on its way.
-template <typename O, int PITCH>
-__device__ __forceinline__ void read_slice(const unsigned char* lds, int row, int lane, bf16x8 (&f)[4][2], std::true_type) {
+// The fragments of one or two neighbouring blocks of 32 rows (from `row` on)
+// over a whole slice of 64. The transposing reads are one piece of assembly
+// that ends with their wait: as the compiler's own loads, each would first wait
+// for every load to LDS still on its way.
+template <typename O, int PITCH, int N>
+__device__ __forceinline__ void read_slice(const unsigned char* lds, int row, int lane, bf16x8 (&f)[4][N], std::true_type) {
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) f[kk][i] = O::frag(lds, row + 32 * i, kk, lane);
+        for (int i = 0; i < N; ++i) {
+            const int r = row + 32 * i + (lane & 31), c = 2 * kk + (lane >> 5);
+            f[kk][i] = *reinterpret_cast<const bf16x8*>(lds + r * PITCH + 16 * (c ^ O::swizzle(r)));
+        }
+}
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+// A lane of a 16-lane group receives element (i mod 4) of the 8 bytes addressed
+// by source lane 4 e + i / 4, e = 0 .. 3: four consecutive k of its row.
+template <typename O, int PITCH>
+__device__ __forceinline__ uint32_t tr_address(const unsigned char* lds, int row, int lane) {
+    const int g = lane >> 4, s = lane & 15;
+    const int k = 8 * (g >> 1) + (s >> 2), r = row + 16 * (g & 1) + 4 * (s & 3);
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)(lds + k * PITCH +
+                                                                                        16 * ((r >> 3) ^ O::swizzle(k)) + 2 * (r & 7));
+}
+__device__ __forceinline__ bf16x8 tr_frag(u32x2 lo, u32x2 hi) {
+    const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
+    return __builtin_bit_cast(bf16x8, v);
+}
+template <typename O, int PITCH>
+__device__ __forceinline__ void read_slice(const unsigned char* lds, int row, int lane, bf16x8 (&f)[4][1], std::false_type) {
+    const uint32_t p = tr_address<O, PITCH>(lds, row, lane);
+    u32x2 x[4][2];   // [k-step][first, second four of eight k]
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%c9\n\t"
+        "ds_read_b64_tr_b16 %2, %8 offset:%c10\n\tds_read_b64_tr_b16 %3, %8 offset:%c11\n\t"
+        "ds_read_b64_tr_b16 %4, %8 offset:%c12\n\tds_read_b64_tr_b16 %5, %8 offset:%c13\n\t"
+        "ds_read_b64_tr_b16 %6, %8 offset:%c14\n\tds_read_b64_tr_b16 %7, %8 offset:%c15\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]), "=&v"(x[3][0]),
+          "=&v"(x[3][1])
+        : "v"(p), "i"(4 * PITCH), "i"(16 * PITCH), "i"(20 * PITCH), "i"(32 * PITCH), "i"(36 * PITCH), "i"(48 * PITCH), "i"(52 * PITCH)
+        : "memory");
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) f[kk][0] = tr_frag(x[kk][0], x[kk][1]);
 }
 template <typename O, int PITCH>
 __device__ __forceinline__ void read_slice(const unsigned char* lds, int row, int lane, bf16x8 (&f)[4][2], std::false_type) {
-    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-    const int g = lane >> 4, s = lane & 15;
-    const int k = 8 * (g >> 1) + (s >> 2), r = row + 16 * (g & 1) + 4 * (s & 3);
-    auto at = [&](int rr) {
-        return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)(lds + k * PITCH + 16 * ((rr >> 3) ^ O::swizzle(k)) + 2 * (rr & 7));
-    };
-    const uint32_t p0 = at(r), p1 = at(r + 32);
+    const uint32_t p0 = tr_address<O, PITCH>(lds, row, lane), p1 = tr_address<O, PITCH>(lds, row + 32, lane);
     u32x2 x[4][2][2];   // [k-step][block][first, second four of eight k]
     asm volatile(
         "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:%c18\n\t"
@@ -557,11 +568,7 @@ __device__ __forceinline__ void read_slice(const unsigned char* lds, int row, in
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-            const u32x4 v = {x[kk][i][0][0], x[kk][i][0][1], x[kk][i][1][0], x[kk][i][1][1]};
-            f[kk][i] = __builtin_bit_cast(bf16x8, v);
-        }
+        for (int i = 0; i < 2; ++i) f[kk][i] = tr_frag(x[kk][i][0], x[kk][i][1]);
 }
 
 // Which tile a block takes: each of the eight dies (blocks go to them in
@@ -577,6 +584,10 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t total, uint32_t tm
     *n = in / h;
 }
 
+// Tiles of 64 or 128 a side for launches that 256 x 256 tiles would not fill
+// the chip with: four waves, several blocks a CU, so that one's MFMAs run while
+// another reads fragments. S - 1 slices are on their way; one barrier a slice
+// says that it has landed for every wave and that the one before it is read.
 template <Product KIND, typename T>
 __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
     constexpr bool AK = KIND != PROD_WEIGHT, BKM = KIND == PROD_FORWARD;
@@ -597,77 +608,40 @@ __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
     OB ob;
     oa.init(static_cast<const uint16_t*>(a.A) + (AK ? m0 * a.lda + k0 : k0 * a.lda + m0), a.lda, a.M - m0, k_end - k0, wave, lane);
     ob.init(static_cast<const uint16_t*>(a.B) + (BKM ? n0 * a.ldb + k0 : k0 * a.ldb + n0), a.ldb, a.N - n0, k_end - k0, wave, lane);
-    auto load = [&](int q, unsigned char* st) {
-        if (q < OA::Q) oa.load(q, st, wave);
-        else ob.load(q - OA::Q, st + T::A_BYTES, wave);
+    auto request = [&](unsigned char* st) {
+#pragma unroll
+        for (int q = 0; q < OA::Q; ++q) oa.load(q, st, wave);
+#pragma unroll
+        for (int q = 0; q < OB::Q; ++q) ob.load(q, st + T::A_BYTES, wave);
+        oa.advance();
+        ob.advance();
     };
     static_assert(OA::Q + OB::Q == T::LOADS, "every load is a whole block of one operand");
 
     f32x16 acc[T::FM][T::FN];
     start_sums<KIND, T>(a, acc, n0 + wn, lane);
-
-    // The k-steps run on over slice ends: a slice's last step reads the next
-    // one's first fragments, so the barrier between them stands among queued
-    // MFMAs. Once a wave holds a slice's last fragments its stage is free.
-    // Slices past the end load zeros (k_left <= 0), so that every iteration
-    // issues and awaits the same number of loads.
-    constexpr int KK = T::BK / 16, NM = T::FM * T::FN;
-    struct Frags { bf16x8 a[T::FM], b[T::FN]; } f[2];
-    auto read = [&](Frags& x, const unsigned char* st, int kk) {
-#pragma unroll
-        for (int i = 0; i < T::FM; ++i) x.a[i] = OA::frag(st, wm + 32 * i, kk, lane);
-#pragma unroll
-        for (int j = 0; j < T::FN; ++j) x.b[j] = OB::frag(st + T::A_BYTES, wn + 32 * j, kk, lane);
-    };
     const int n = s1 - s0;
 #pragma unroll
-    for (int p = 0; p < T::S; ++p) {
-#pragma unroll
-        for (int q = 0; q < T::LOADS; ++q) load(q, lds + p * T::STAGE);
-        oa.advance();
-        ob.advance();
-    }
-    wait_loads<(T::S - 1) * T::LOADS>();
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    read(f[0], lds, 0);
+    for (int p = 0; p < T::S - 1; ++p) request(lds + p * T::STAGE);
     for (int s = 0; s < n; ++s) {
-        unsigned char* st = lds + s % T::S * T::STAGE;
-        const unsigned char* next = lds + (s + 1) % T::S * T::STAGE;
+        // slices past the end are requested too (zeros): the count stays exact
+        wait_vmcnt<(T::S - 2) * T::LOADS>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const unsigned char* st = lds + s % T::S * T::STAGE;
+        bf16x8 fa[4][T::FM], fb[4][T::FN];
+        read_slice<OA, OA::PITCH>(st, wm, lane, fa, std::bool_constant<AK>{});
+        read_slice<OB, OB::PITCH>(st + T::A_BYTES, wn, lane, fb, std::bool_constant<BKM>{});
+        __builtin_amdgcn_sched_barrier(0);
+        request(lds + (s + T::S - 1) % T::S * T::STAGE);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kk = 0; kk < KK - 1; ++kk) {
-            read(f[(kk + 1) & 1], st, kk + 1);
+        for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
             for (int i = 0; i < T::FM; ++i)
 #pragma unroll
                 for (int j = 0; j < T::FN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[kk & 1].b[j], f[kk & 1].a[i], acc[i][j], 0, 0, 0);
-        }
-        // the slice's last fragments are in registers, and the next slice has
-        // landed: behind the barrier that holds for all waves
-        __builtin_amdgcn_sched_barrier(0);
-        wait_loads<(T::S - 2) * T::LOADS>();
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        read(f[0], next, 0);
-#pragma unroll
-        for (int i = 0; i < T::FM; ++i)
-#pragma unroll
-            for (int j = 0; j < T::FN; ++j) {
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[(KK - 1) & 1].b[j], f[(KK - 1) & 1].a[i], acc[i][j], 0, 0, 0);
-                // the freed stage's loads, spread over the MFMAs: in one burst
-                // they would hold the wave in the issue queue
-#pragma unroll
-                for (int q = 0; q < T::LOADS; ++q)
-                    if (q * NM / T::LOADS == i * T::FN + j) {
-                        __builtin_amdgcn_sched_barrier(0);
-                        load(q, st);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-            }
-        oa.advance();
-        ob.advance();
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[kk][j], fa[kk][i], acc[i][j], 0, 0, 0);
     }
     finish_sums<KIND, T>(a, acc, lds, m0 + wm, n0 + wn, m0 + T::BM <= a.M && n0 + T::BN <= a.N, wave, lane);
 }
@@ -888,9 +862,10 @@ __global__ __launch_bounds__(64) void product_join(ProductArgs a) {
     });
 }
 
-typedef Tile<128, 128, 64, 2, 2, 2> SmallTile;
+typedef Tile<128, 128, 64, 2, 2, 2> MiddleTile;
+typedef Tile<64, 64, 64, 4, 2, 2> SmallTile;
 
-enum Form { FORM_ANY, FORM_ANY_64, FORM_FEW, FORM_SMALL, FORM_BIG };
+enum Form { FORM_ANY, FORM_ANY_64, FORM_FEW, FORM_SMALL, FORM_MIDDLE, FORM_BIG };
 struct Plan {
     Form form;
     int splits;
@@ -909,31 +884,60 @@ bool whole_chunks(Product kind, const ProductArgs& a) {
 
 int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
 
-// Parts of K that bring a launch to about `blocks` blocks, each of `least` of
-// K or more.
-int splits_for(int64_t tiles, int64_t K, int64_t blocks, int64_t least) {
-    return (int)std::max<int64_t>(1, std::min<int64_t>({blocks / std::max<int64_t>(tiles, 1), K / least, 32}));
+// A launch's time by its tiles: 256 CUs take up to `most` tiles each at a time,
+// and such a round lasts `fixed` us (the start and the epilogue) plus, for every
+// 64 of K, unit[n - 1] us where a CU holds n tiles. Measured in graphs of 30
+// calls at 64 to 4096 tokens, rows and columns; the model is within a fifth of
+// the measurements, the forms it decides between are often twice apart:
+//   1024 x 1024, K 1024:  64 6.2, 128 12.0 us;  1024 x 2048:  8.6, 12.4
+//   2048 x 4096, K 1024:  64 30, 128 21.8, 256 28.6
+//   2048 x 8192, K 2048:  64 107, 128 69, 256 58.7
+// A product cut into parts adds their round trip through memory at 4 TB/s and
+// a launch: 2048 x 2048, K 8192 on 128 x 128 tiles 86.6 whole, 73.3 in two;
+// 64 x 2048, K 8192 on 64 x 64 tiles 28 whole, 13.2 in eight.
+struct Cost {
+    int tile, most;
+    double fixed, unit[4];
+};
+constexpr Cost kSmallCost = {64, 2, 2.7, {0.2, 0.38}};
+constexpr Cost kMiddleCost = {128, 2, 5.5, {0.65, 0.93}};
+constexpr Cost kBigCost = {256, 1, 10.0, {1.5}};
+constexpr Cost kAny64Cost[2] = {{64, 4, 2.7, {2.3, 3.2, 4.3, 5.5}}, {64, 4, 2.7, {0.6, 0.9, 1.05, 1.2}}};   // fp32, bf16
+constexpr Cost kAnyCost[2] = {{128, 2, 4.0, {6.1, 10.4}}, {128, 2, 4.0, {1.5, 2.0}}};
+
+double time_of(const Cost& c, const ProductArgs& a, int splits) {
+    const int64_t tiles = tiles_of(a.M, a.N, c.tile, c.tile) * splits;
+    const double units = (double)((a.K + 63) / 64) / splits;
+    const int64_t rounds = tiles / (256 * c.most), left = (tiles % (256 * c.most) + 255) / 256;
+    double t = rounds * (c.fixed + units * c.unit[c.most - 1]);
+    if (left) t += c.fixed + units * c.unit[left - 1];
+    if (splits > 1) t += 3.0 + (double)splits * a.M * a.N * 8 / 4e6;
+    return t;
 }
 
 Plan plan_of(Product kind, const ProductArgs& a) {
-    Plan p{FORM_ANY, 1};
-    const int64_t tiles = tiles_of(a.M, a.N, 128, 128);
-    if (!whole_chunks(kind, a)) {
-        if (tiles < 128) {
-            p.form = FORM_ANY_64;
-            p.splits = splits_for(tiles_of(a.M, a.N, 64, 64), a.K, 512, 128);
-        } else {
-            p.splits = splits_for(tiles, a.K, 512, 256);
+    Plan best{FORM_FEW, 1};
+    const bool whole = whole_chunks(kind, a);
+    if (whole && kind == PROD_FORWARD && a.M <= 32) return best;
+    double least = 0.0;
+    auto offer = [&](Form form, const Cost& c) {
+        for (int splits = 1; splits <= 32 && (splits == 1 || (a.K + 63) / 64 >= splits); splits *= 2) {
+            const double t = time_of(c, a, splits);
+            if (best.form == FORM_FEW || t < least) {
+                best = {form, splits};
+                least = t;
+            }
         }
-    } else if (kind == PROD_FORWARD && a.M <= 32) {
-        p.form = FORM_FEW;
-    } else if (tiles_of(a.M, a.N, 256, 256) >= 128) {
-        p.form = FORM_BIG;
+    };
+    if (whole) {
+        offer(FORM_BIG, kBigCost);
+        offer(FORM_MIDDLE, kMiddleCost);
+        offer(FORM_SMALL, kSmallCost);
     } else {
-        p.form = FORM_SMALL;
-        p.splits = splits_for(tiles, a.K, 512, 256);
+        offer(FORM_ANY, kAnyCost[a.bf16]);
+        offer(FORM_ANY_64, kAny64Cost[a.bf16]);
     }
-    return p;
+    return best;
 }
 
 template <typename T, typename F>
@@ -965,6 +969,7 @@ hipError_t launch_kind(const ProductArgs& a, Form form, hipStream_t s) {
     hipError_t e = hipSuccess;
     if constexpr (std::is_same<T, uint16_t>::value) {
         if (form == FORM_BIG) e = launch_tiles<PairTile>(&product_pairs<KIND>, a, s);
+        else if (form == FORM_MIDDLE) e = launch_tiles<MiddleTile>(&product_tiles<KIND, MiddleTile>, a, s);
         else if (form == FORM_SMALL) e = launch_tiles<SmallTile>(&product_tiles<KIND, SmallTile>, a, s);
         else if (form == FORM_FEW) return launch_few(a, s);
     }
