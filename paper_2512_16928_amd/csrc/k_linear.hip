@@ -17,6 +17,8 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) short i16x4;
 typedef __attribute__((ext_vector_type(8))) short i16x8;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 // ------------------------------------------------------------- the epilogue
@@ -477,6 +479,46 @@ __device__ __forceinline__ void start_sums(const ProductArgs& a, f32x16 (&acc)[T
     }
 }
 
+// The bias gradient beside PROD_WEIGHT: sums over k of A's rows, from the
+// fragments that are in registers anyway. The waves that share rows (the tiles
+// of a row of tiles, WN waves each) take a slice each in turn; what they have is
+// a row of partial sums each, added up in order by a launch of its own.
+template <typename T>
+struct RowSums {
+    float sum[T::FM];
+    int turn, turns;   // slices until this wave's next, and from one to the next
+    __device__ __forceinline__ void init(const ProductArgs& a, uint32_t in, uint32_t tn, int wn, int s0) {
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) sum[i] = 0.0f;
+        turns = (int)tn * T::WN;
+        turn = (int)(((int64_t)(wn * tn + in) - s0 % turns + turns) % turns);
+        if (!a.row_sums) turn = turns = 0x7fffffff;
+    }
+    template <int N>
+    __device__ __forceinline__ void add(const bf16x8 (&f)[4][N], int first) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                const u32x4 w = __builtin_bit_cast(u32x4, f[kk][i]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sum[first + i] += __uint_as_float(w[q] << 16) + __uint_as_float(w[q] & 0xffff0000u);
+            }
+    }
+    __device__ __forceinline__ bool mine() const { return turn == 0; }
+    __device__ __forceinline__ void next() { turn = turn == 0 ? turns - 1 : turn - 1; }
+    __device__ __forceinline__ void store(const ProductArgs& a, uint32_t in, uint32_t tn, int wn, int64_t m0, int lane) {
+        if (!a.row_sums) return;
+        float* p = a.row_sums + (((int64_t)blockIdx.y * T::WN + wn) * tn + in) * a.M;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+            const float v = sum[i] + __shfl_xor(sum[i], 32);   // the halves of a wave have different k
+            const int64_t m = m0 + 32 * i + (lane & 31);
+            if (lane < 32 && m < a.M) stg(p + m, v);
+        }
+    }
+};
+
 // The end of a wave's sums: parts as they are, else finished through LDS.
 template <Product KIND, typename T>
 __device__ __forceinline__ void finish_sums(const ProductArgs& a, const f32x16 (&acc)[T::FM][T::FN], unsigned char* lds, int64_t m0,
@@ -513,8 +555,6 @@ __device__ __forceinline__ void read_slice(const unsigned char* lds, int row, in
             f[kk][i] = *reinterpret_cast<const bf16x8*>(lds + r * PITCH + 16 * (c ^ O::swizzle(r)));
         }
 }
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 // A lane of a 16-lane group receives element (i mod 4) of the 8 bytes addressed
 // by source lane 4 e + i / 4, e = 0 .. 3: four consecutive k of its row.
 template <typename O, int PITCH>
@@ -620,6 +660,8 @@ __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
 
     f32x16 acc[T::FM][T::FN];
     start_sums<KIND, T>(a, acc, n0 + wn, lane);
+    RowSums<T> rows;
+    if constexpr (!AK) rows.init(a, in, tn, wave % T::WN, s0);
     const int n = s1 - s0;
 #pragma unroll
     for (int p = 0; p < T::S - 1; ++p) request(lds + p * T::STAGE);
@@ -642,7 +684,12 @@ __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
 #pragma unroll
                 for (int j = 0; j < T::FN; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[kk][j], fa[kk][i], acc[i][j], 0, 0, 0);
+        if constexpr (!AK) {
+            if (rows.mine()) rows.add(fa, 0);
+            rows.next();
+        }
     }
+    if constexpr (!AK) rows.store(a, in, tn, wave % T::WN, m0 + wm, lane);
     finish_sums<KIND, T>(a, acc, lds, m0 + wm, n0 + wn, m0 + T::BM <= a.M && n0 + T::BN <= a.N, wave, lane);
 }
 
@@ -720,6 +767,9 @@ __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a
     f32x16 acc[T::FM][T::FN];
     start_sums<KIND, T>(a, acc, n0 + wn * T::TN, lane);
 
+    RowSums<T> rows;
+    if constexpr (!AK) rows.init(a, in, tn, wn, s0);
+
     request_first(lds);
     request_second(lds);
     request_first(lds + T::STAGE);
@@ -740,6 +790,9 @@ __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
                     acc[2 * h + i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[kk][j], fa[kk][i], acc[2 * h + i][j], 0, 0, 0);
+        if constexpr (!AK) {
+            if (rows.mine()) rows.add(fa, 2 * h);
+        }
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         if (!second) wait_vmcnt<8>();
@@ -771,8 +824,10 @@ __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a
         read_a(st + T::HALF_A);
         end_reads();
         compute(std::integral_constant<int, 1>{});
+        if constexpr (!AK) rows.next();
     }
     if (!second) swap();
+    if constexpr (!AK) rows.store(a, in, tn, wn, m0 + wm * T::TM, lane);
     finish_sums<KIND, T>(a, acc, lds, m0 + wm * T::TM, n0 + wn * T::TN, m0 + T::BM <= a.M && n0 + T::BN <= a.N, wave, lane);
 }
 
@@ -993,12 +1048,20 @@ size_t part_bytes(const ProductArgs& a, int splits) {
 
 size_t product_workspace(Product kind, const ProductArgs& a) { return part_bytes(a, plan_of(kind, a).splits); }
 
+int64_t product_row_sums(const ProductArgs& a) {
+    const Plan p = plan_of(PROD_WEIGHT, a);
+    const int tile = p.form == FORM_BIG ? 256 : p.form == FORM_MIDDLE ? 128 : p.form == FORM_SMALL ? 64 : 0;
+    const int waves = p.form == FORM_BIG ? PairTile::WN : 2;
+    return tile ? (int64_t)p.splits * waves * ((a.N + tile - 1) / tile) : 0;
+}
+
 size_t product_workspace_most(Product kind, int64_t M, int64_t N, int64_t K, int bf16) {
     // the most over what pointers and pitches can make of it: chunks whole or not
     ProductArgs a{};
     a.M = M; a.N = N; a.K = K; a.bf16 = bf16;
     a.lda = a.ldb = 8;
-    const size_t whole = product_workspace(kind, a);
+    const size_t sums = kind == PROD_WEIGHT ? (size_t)product_row_sums(a) * M * 4 : 0;
+    const size_t whole = product_workspace(kind, a) + sums;
     a.lda = 1;
     return std::max(whole, product_workspace(kind, a));
 }

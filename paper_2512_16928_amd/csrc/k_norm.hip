@@ -634,6 +634,10 @@ hipError_t launch_col_sum(const ColSumArgs& a, hipStream_t s) {
     else col_parts<float, 0><<<grid, kThreads, 0, s>>>(a, a.width);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+    return launch_col_join(a, s);
+}
+
+hipError_t launch_col_join(const ColSumArgs& a, hipStream_t s) {
     return join({a.part, a.blocks, a.width, a.width, a.width, a.out, nullptr, a.out_bf16, a.accumulate}, s);
 }
 

@@ -195,8 +195,13 @@ struct ProductArgs {
     int accumulate;
     float* part;        // partial sums: product_workspace bytes
     int splits;         // set by launch_product
+    float* row_sums;    // nullable, PROD_WEIGHT: [product_row_sums(a)][M], partial sums
+                        // over k of A's rows (the bias gradient's)
 };
-// Bytes of workspace of this call, and the most of any call of these sizes.
+// How many rows of row_sums PROD_WEIGHT gives; 0 where its form gives none.
+int64_t product_row_sums(const ProductArgs& a);
+// Bytes of workspace of this call without row_sums, and the most of any call of
+// these sizes, with them.
 size_t product_workspace(Product kind, const ProductArgs& a);
 size_t product_workspace_most(Product kind, int64_t M, int64_t N, int64_t K, int bf16);
 hipError_t launch_product(Product kind, ProductArgs a, hipStream_t s);
@@ -224,6 +229,8 @@ struct ColSumArgs {
 };
 int64_t col_sum_blocks(int64_t tokens, int64_t width);
 hipError_t launch_col_sum(const ColSumArgs& a, hipStream_t s);
+// The second half alone: out from part [blocks][width].
+hipError_t launch_col_join(const ColSumArgs& a, hipStream_t s);
 
 struct NormArgs {
     const void* X;

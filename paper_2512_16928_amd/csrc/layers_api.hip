@@ -158,13 +158,12 @@ int take_scratch(const dion2_layer_options& o, size_t bytes, hipStream_t s, Scra
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
-int run_product(Product kind, ProductArgs& a, const dion2_layer_options& o, size_t more, Scratch* ws, hipStream_t s) {
+int run_product(Product kind, ProductArgs& a, const dion2_layer_options& o, hipStream_t s) {
     a.bf16 = o.dtype == DION2_DTYPE_BF16;
-    const size_t part = product_workspace(kind, a);
-    int st = take_scratch(o, part + more, s, ws);
+    Scratch ws;
+    int st = take_scratch(o, product_workspace(kind, a), s, &ws);
     if (st != DION2_OK) return st;
-    a.part = reinterpret_cast<float*>(ws->p);
-    ws->p += part;
+    a.part = reinterpret_cast<float*>(ws.p);
     hipError_t e = launch_product(kind, a, s);
     return e == hipSuccess ? DION2_OK : hip_fail(e, "launch of a linear layer's product");
 }
@@ -192,8 +191,7 @@ int linear_forward(void* Y, const void* X, const void* W, const void* bias, cons
     a.R = R; a.ldr = ldr;
     a.Z = Z; a.ldz = ldz;
     a.act = o.act;
-    Scratch ws;
-    return run_product(PROD_FORWARD, a, o, 0, &ws, s);
+    return run_product(PROD_FORWARD, a, o, s);
 }
 
 int linear_backward_input(void* dX, const void* dY, const void* W, const void* Z, int64_t tokens, int64_t rows,
@@ -218,8 +216,7 @@ int linear_backward_input(void* dX, const void* dY, const void* W, const void* Z
     a.out = dX; a.ldo = lddx;
     a.Z = const_cast<void*>(Z); a.ldz = ldz;
     a.act = o.act;
-    Scratch ws;
-    return run_product(PROD_INPUT, a, o, 0, &ws, s);
+    return run_product(PROD_INPUT, a, o, s);
 }
 
 int linear_backward_weight(void* G, void* dbias, const void* dY, const void* X, int64_t tokens, int64_t rows,
@@ -236,24 +233,31 @@ int linear_backward_weight(void* G, void* dbias, const void* dY, const void* X, 
     ColSumArgs c{};
     c.X = dY; c.ldx = lddy; c.tokens = tokens; c.width = rows;
     c.bf16 = o.dtype == DION2_DTYPE_BF16;
-    c.blocks = col_sum_blocks(tokens, rows);
     c.out = dbias; c.out_bf16 = o.g_dtype == DION2_DTYPE_BF16; c.accumulate = o.accumulate != 0;
-    const size_t sums = dbias ? align256((size_t)c.blocks * rows * 4) : 0;
+    ProductArgs a{};
+    a.A = dY; a.lda = lddy;
+    a.B = X; a.ldb = ldx;
+    a.M = rows; a.N = cols; a.K = tokens;
+    a.out = G; a.ldo = cols; a.out_bf16 = c.out_bf16;
+    a.accumulate = c.accumulate;
+    a.bf16 = c.bf16;
+    // the bias gradient's partial sums come out of the product where its form
+    // gives them, else out of a pass of their own
+    const int64_t beside = G && dbias ? product_row_sums(a) : 0;
+    c.blocks = beside ? beside : col_sum_blocks(tokens, rows);
+    const size_t part = G ? align256(product_workspace(PROD_WEIGHT, a)) : 0;
     Scratch ws;
+    st = take_scratch(o, part + (dbias ? align256((size_t)c.blocks * rows * 4) : 0), s, &ws);
+    if (st != DION2_OK) return st;
+    c.part = reinterpret_cast<float*>(ws.p + part);
+    hipError_t err = hipSuccess;
     if (G) {
-        ProductArgs a{};
-        a.A = dY; a.lda = lddy;
-        a.B = X; a.ldb = ldx;
-        a.M = rows; a.N = cols; a.K = tokens;
-        a.out = G; a.ldo = cols; a.out_bf16 = c.out_bf16;
-        a.accumulate = c.accumulate;
-        st = run_product(PROD_WEIGHT, a, o, sums, &ws, s);
-    } else {
-        st = take_scratch(o, sums, s, &ws);
+        a.part = reinterpret_cast<float*>(ws.p);
+        a.row_sums = beside ? c.part : nullptr;
+        err = launch_product(PROD_WEIGHT, a, s);
+        if (err != hipSuccess) return hip_fail(err, "launch of a linear layer's product");
     }
-    if (st != DION2_OK || !dbias) return st;
-    c.part = reinterpret_cast<float*>(ws.p);
-    hipError_t err = launch_col_sum(c, s);
+    if (dbias) err = beside ? launch_col_join(c, s) : launch_col_sum(c, s);
     return err == hipSuccess ? DION2_OK : hip_fail(err, "launch of the bias gradient");
 }
 
@@ -392,10 +396,10 @@ size_t dion2_linear_workspace_size(int64_t tokens, int64_t rows, int64_t cols, c
     const dion2_layer_options o = options_of(opt);
     if (check_options(o) != DION2_OK || check_sizes(tokens, rows, cols) != DION2_OK) return 0;
     const int bf16 = o.dtype == DION2_DTYPE_BF16;
-    const size_t weight = product_workspace_most(PROD_WEIGHT, rows, cols, tokens, bf16) +
+    const size_t weight = align256(product_workspace_most(PROD_WEIGHT, rows, cols, tokens, bf16)) +
                           align256((size_t)col_sum_blocks(tokens, rows) * rows * 4);
-    return std::max({product_workspace_most(PROD_FORWARD, tokens, rows, cols, bf16),
-                     product_workspace_most(PROD_INPUT, tokens, cols, rows, bf16), weight});
+    return std::max({align256(product_workspace_most(PROD_FORWARD, tokens, rows, cols, bf16)),
+                     align256(product_workspace_most(PROD_INPUT, tokens, cols, rows, bf16)), weight});
 }
 
 size_t dion2_layernorm_workspace_size(int64_t tokens, int64_t cols, const dion2_layer_options* opt) {
