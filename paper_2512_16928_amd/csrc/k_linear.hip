@@ -132,16 +132,31 @@ template <typename T, int GT> struct GSlice;
 template <int GT> struct GSlice<uint16_t, GT> { static constexpr int K = 4096 / GT, BYTES = GT * K * 2; };
 template <int GT> struct GSlice<float, GT> { static constexpr int K = 2048 / GT, LD = GT + 4, BYTES = K * LD * 4; };
 
-__device__ __forceinline__ uint4 load_chunk(const uint16_t* p, int n) {
+// The n entries (1 to all of a chunk's) from p on, zeros behind them. `before`
+// entries of the row lie before p: with enough of them a chunk that the row's
+// end cuts is read as the row's last 16 bytes, and the entries before it dropped.
+__device__ __forceinline__ uint4 load_chunk(const uint16_t* p, int n, int64_t before = 0) {
     if (n >= 8) return ldg<uint4>(p);
+    if (before >= 8 - n) {
+        const uint4 v = ldg<uint4>(p - (8 - n));
+        const uint64_t lo = (uint64_t)v.y << 32 | v.x, hi = (uint64_t)v.w << 32 | v.z;
+        const int b = 16 * (-n & 3);   // 8 - n entries: whole quads of them and b bits
+        const uint64_t carry = b ? hi << (64 - b) : 0;
+        const uint64_t l = n > 4 ? lo >> b | carry : hi >> b, h = n > 4 ? hi >> b : 0;
+        return make_uint4((uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32));
+    }
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < n) w[i / 2] |= (uint32_t)ldg<uint16_t>(p + i) << (16 * (i & 1));
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ uint4 load_chunk(const float* p, int n) {
+__device__ __forceinline__ uint4 load_chunk(const float* p, int n, int64_t before = 0) {
     if (n >= 4) return ldg<uint4>(p);
+    if (before >= 4 - n) {
+        const uint4 v = ldg<uint4>(p - (4 - n));
+        return n == 3 ? make_uint4(v.y, v.z, v.w, 0) : n == 2 ? make_uint4(v.z, v.w, 0, 0) : make_uint4(v.w, 0, 0, 0);
+    }
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -169,7 +184,7 @@ struct GOperand {
             const int64_t n_outer = KMAJOR ? rows : K, n_inner = KMAJOR ? K : rows;
             const int64_t left = n_inner - inner;
             const int n = outer < n_outer ? (int)(left < E ? left : E) : 0;
-            reg[q] = n > 0 ? load_chunk(p + outer * ld + inner, n) : make_uint4(0, 0, 0, 0);
+            reg[q] = n > 0 ? load_chunk(p + outer * ld + inner, n, inner) : make_uint4(0, 0, 0, 0);
         }
     }
     __device__ __forceinline__ void stage(unsigned char* lds, int tid) const {
