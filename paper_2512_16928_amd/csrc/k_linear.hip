@@ -629,7 +629,7 @@ __device__ __forceinline__ void read_slice(const unsigned char* lds, int row, in
 // Which tile a block takes: each of the eight dies (blocks go to them in
 // turn) gets neighbouring ones, in columns of kGroup tiles of m, so that its
 // L2 holds the operand rows its blocks share.
-constexpr int kDies = 8, kGroup = 8;
+constexpr int kDies = 8, kGroup = 4;
 __device__ __forceinline__ void tile_of(uint32_t id, uint32_t total, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
     const uint32_t q = total / kDies, r = total % kDies, die = id % kDies;
     const uint32_t at = die * q + (die < r ? die : r) + id / kDies;
@@ -829,14 +829,20 @@ __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a
     for (int s = 0; s < n; ++s) {
         unsigned char* st = lds + (s & 1) * T::STAGE;
         unsigned char* other = lds + T::STAGE - (s & 1) * T::STAGE;
-        request_second(other);
+        // requests go out while reads are waited for: behind reads that the
+        // compiler waits for, ahead of those that end with their wait
+        if constexpr (!BKM) request_second(other);
         if constexpr (AK) read_a(st);
         read_slice<OB, OB::PITCH>(st + 2 * T::HALF_A, wn * T::TN, lane, fb, std::bool_constant<BKM>{});
         if constexpr (!AK) read_a(st);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (BKM) request_second(other);
         end_reads();
         compute(std::integral_constant<int, 0>{});
-        request_first(st);
+        if constexpr (!AK) request_first(st);
         read_a(st + T::HALF_A);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (AK) request_first(st);
         end_reads();
         compute(std::integral_constant<int, 1>{});
         if constexpr (!AK) rows.next();
