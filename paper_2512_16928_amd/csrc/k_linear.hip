@@ -859,7 +859,7 @@ __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a
 // block's waves share 16 rows, each a run of k, and add up in LDS.
 template <int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void product_few(ProductArgs a) {
-    constexpr int U = NT == 1 ? 8 : 4;    // k-steps whose loads are on their way together
+    constexpr int U = NT == 1 ? (WAVES == 4 ? 16 : 8) : 4;   // k-steps whose loads are on their way together
     typedef __attribute__((ext_vector_type(4))) float f32x4;
     __shared__ __align__(16) float part[WAVES][NT][16][20];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -1031,12 +1031,14 @@ hipError_t launch_any(const ProductArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// One token through 8192 x 2048: four waves a block 7.9 us, eight 8.3, sixteen
+// 10.3; through 2048 x 8192, where sixteen are needed to have as many loads on
+// their way, 12.0.
 hipError_t launch_few(const ProductArgs& a, hipStream_t s) {
     const unsigned blocks = (unsigned)((a.N + 15) / 16);
-    // sixteen waves where a run of k still is eight loads of each
     if (a.M > 16) product_few<2, 8><<<blocks, 512, 0, s>>>(a);
-    else if (a.K >= 16 * 8 * 32) product_few<1, 16><<<blocks, 1024, 0, s>>>(a);
-    else product_few<1, 8><<<blocks, 512, 0, s>>>(a);
+    else if (blocks < 256 && a.K >= 4096) product_few<1, 16><<<blocks, 1024, 0, s>>>(a);
+    else product_few<1, 4><<<blocks, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
