@@ -429,8 +429,9 @@ int dion2_plan_form(int batch, int64_t rows, int64_t cols, float alpha,
  * says so it may be exactly the same matrix (pointer and pitch). Column
  * slices of one buffer with equal pitches do not overlap. The stream's
  * device must be the current one. Limits: 0 <= tokens < 2^31, rows and cols as
- * for the step, pitches below 2^28, and tokens / 128 times the longer of rows
- * and cols / 128 below 2^24 (DION2_ERR_UNSUPPORTED otherwise). Calls may be captured in a HIP graph; one that
+ * for the step, pitches below 2^28, and fewer than 2^24 tiles of 64 x 64 in
+ * tokens times the longer of rows and cols (DION2_ERR_UNSUPPORTED otherwise;
+ * 6.9e10 entries, 128 GB of bf16). Calls may be captured in a HIP graph; one that
  * needs a workspace (dion2_linear_workspace_size,
  * dion2_layernorm_workspace_size) then needs the caller's, since a graph
  * may be replayed while the library's is in use or has been moved:

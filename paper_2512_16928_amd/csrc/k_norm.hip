@@ -154,8 +154,10 @@ __global__ __launch_bounds__(64 * row_waves(WPR)) void norm_regs(NormArgs a) {
     int turn = 0;
     const int cols = (int)a.cols;
     const float inv = 1.0f / (float)cols;
-    const int64_t t = (int64_t)blockIdx.x * RPB + threadIdx.x / 64 / WPR;
-    if (RPB > 1 && t >= a.tokens) return;   // whole waves
+    // a row a wave, or a block; the grid has a second dimension because a
+    // launch's threads fit 32 bits in each
+    const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * RPB + threadIdx.x / 64 / WPR;
+    if (t >= a.tokens) return;   // whole waves, or the whole block
     R x;
     x.load(static_cast<const T*>(a.X) + t * a.ldx, cols);
     float s = 0.0f, none = 0.0f, v[8];
@@ -669,7 +671,9 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
             norm_rows<typename R::T><<<row_grid(a.tokens), kThreads, 0, s>>>(a);
         } else {
             constexpr int WAVES = row_waves(R::WPR), RPB = WAVES / R::WPR;
-            norm_regs<typename R::T, R::WPR, R::CH, R::RAGGED><<<(unsigned)((a.tokens + RPB - 1) / RPB), 64 * WAVES, 0, s>>>(a);
+            const int64_t blocks = (a.tokens + RPB - 1) / RPB, x = std::min<int64_t>(blocks, 1 << 20);
+            const dim3 grid((unsigned)x, (unsigned)((blocks + x - 1) / x));
+            norm_regs<typename R::T, R::WPR, R::CH, R::RAGGED><<<grid, 64 * WAVES, 0, s>>>(a);
         }
         return hipGetLastError();
     });

@@ -122,9 +122,9 @@ int check_sizes(int64_t tokens, int64_t rows, int64_t cols) {
     if (rows > kMaxDim || cols > kMaxDim || rows * cols >= (int64_t(1) << 31))
         return fail(DION2_ERR_UNSUPPORTED, "%lld x %lld: sides up to 2^20 and below 2^31 entries are supported",
                     (long long)rows, (long long)cols);
-    // a launch's threads are counted in 32 bits
+    // a launch's threads are counted in 32 bits: 256 for a tile of 64 x 64
     const int64_t width = std::max(rows, cols);
-    if (((tokens + 127) / 128) * ((width + 127) / 128) >= (int64_t(1) << 24) - 1)
+    if (((tokens + 63) / 64) * ((width + 63) / 64) >= (int64_t(1) << 24))
         return fail(DION2_ERR_UNSUPPORTED, "%lld tokens of %lld entries are more than one launch takes", (long long)tokens,
                     (long long)width);
     return DION2_OK;

@@ -538,6 +538,19 @@ def test_rows_past_2_31_entries(hip_device):
     near(G, want, (t + 16) * 2.0 ** -23 * (dY[-300:].double().abs().t() @ X[-300:].double().abs()), F32, "G")
 
 
+def test_more_rows_than_a_launch_has_blocks(hip_device):
+    """2^26 + 5 short rows: as many waves as would pass a launch's 2^32 threads."""
+    t, c = (1 << 26) + 5, 8
+    X = torch.zeros((t, c), dtype=BF, device="cuda")
+    ends = torch.randn((64, c), generator=gen_of("rows"), device="cuda").to(BF)
+    X[:64], X[-64:] = ends, ends
+    binding.dion2_layernorm_forward(X, X, eps=EPS)
+    want = torch.empty_like(ends)
+    binding.dion2_layernorm_forward(want, ends, eps=EPS)
+    assert torch.equal(X[:64], want) and torch.equal(X[-64:], want)
+    assert bool((X[64:-64] == 0).all())
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_a_block_trains_with_the_step(hip_device, dtype):
     """x + W2 gelu(W1 norm(x) + b1) + b2, forward and backward by these calls and then the step on both matrices: the

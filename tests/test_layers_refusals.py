@@ -89,6 +89,8 @@ CALLS = {"dion2_linear_forward": FORWARD, "dion2_linear_backward_input": INPUT,
     ("dion2_linear_forward", dict(rows=1 << 21, cols=8), {}, DION2_ERR_UNSUPPORTED, "sides"),
     ("dion2_linear_forward", dict(rows=1 << 16, cols=1 << 16), {}, DION2_ERR_UNSUPPORTED, "entries"),
     ("dion2_linear_forward", dict(tokens=(1 << 31) - 1, rows=1, cols=1), {}, DION2_ERR_UNSUPPORTED, "one launch"),
+    ("dion2_linear_forward", dict(tokens=1 << 30, rows=64, cols=8), {}, DION2_ERR_UNSUPPORTED, "one launch"),
+    ("dion2_layernorm_forward", dict(tokens=1 << 30), {}, DION2_ERR_UNSUPPORTED, "one launch"),
     ("dion2_linear_forward", {}, dict(ld_x=79), DION2_ERR_INVALID_ARG, "pitch of X"),
     ("dion2_linear_forward", {}, dict(ld_y=95), DION2_ERR_INVALID_ARG, "pitch of Y"),
     ("dion2_linear_forward", {}, dict(ld_z=-1), DION2_ERR_INVALID_ARG, "pitch of Z"),
