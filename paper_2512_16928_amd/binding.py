@@ -474,25 +474,28 @@ def dion2_plan_info(rows, cols, alpha, axis=AXIS_AUTO):
 
 # ---- the layers around the step
 
+_TYPES = tuple(_DT)
+
+
 def _rows(name, t, shape, dtype, device):
     """A matrix of activations: unit stride along a row, any distance between rows. Returns
     (pointer, pitch); (None, 0) for None."""
     if t is None:
         return None, 0
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}, got {t.device}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
     step, unit = t.stride()
-    if shape[1] > 1 and unit != 1:
+    rows, width = shape
+    if unit != 1 and width > 1:
         raise ValueError(f"{name} must have unit stride along its rows")
-    if shape[0] > 1:
-        if step < shape[1]:
-            raise ValueError(f"{name}'s rows must not overlap")
-    else:
+    if rows <= 1:
         step = 0
+    elif step < width:
+        raise ValueError(f"{name}'s rows must not overlap")
     return t.data_ptr(), step
 
 
@@ -500,12 +503,12 @@ def _whole(name, t, shape, dtypes, device):
     """A contiguous tensor of one of the given types. Returns its pointer; None for None."""
     if t is None:
         return None
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}, got {t.device}")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
@@ -514,9 +517,9 @@ def _whole(name, t, shape, dtypes, device):
 def _matrix(name, t):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name} must be a HIP device tensor, got {t.device}")
-    if t.dtype not in _DT:
+    if t.dtype not in _TYPES:
         raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
     if t.dim() != 2:
         raise ValueError(f"{name} must have 2 dimensions, got {tuple(t.shape)}")
@@ -536,26 +539,29 @@ def _layer_options(dtype, workspace, device):
     return opt
 
 
-def _one_type(what, *tensors):
-    """The common dtype code of those that are not None (bf16 without any)."""
-    kinds = {t.dtype for t in tensors if t is not None}
-    if len(kinds) > 1:
+def _one_type(what, a, b=None):
+    """The common dtype code of those that are not None (bf16 without any); other types are refused
+    where the tensors themselves are checked."""
+    if a is None:
+        a = b
+    elif b is not None and a.dtype is not b.dtype:
         raise ValueError(f"{what} must have one dtype")
-    return _DT[kinds.pop()] if kinds else DTYPE_BF16
+    return DTYPE_BF16 if a is None else _DT.get(a.dtype, DTYPE_BF16)
 
 
 def _layer_call(fn, device, stream, *args):
     """The call with its tensors' device current, on the given stream or that device's current one."""
+    index = device.index
     if stream is None:
-        ptr = torch._C._cuda_getCurrentRawStream(device.index)   # current_stream() without the object
+        ptr = torch._C._cuda_getCurrentRawStream(index)   # current_stream() without the object
     else:
         ptr = stream.cuda_stream
-    if device.index != torch.cuda.current_device():
+    if index != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             status = fn(*args, ptr)
     else:
         status = fn(*args, ptr)
-    if status != DION2_OK:
+    if status:
         _check(status)
 
 
@@ -577,7 +583,7 @@ def dion2_linear_forward(Y, X, W, *, bias=None, residual=None, Z=None, act=ACT_N
     z, opt.ld_z = _rows("Z", Z, shape, dt, dev)
     r, opt.ld_r = _rows("residual", residual, shape, dt, dev)
     _layer_call(load().dion2_linear_forward, dev, stream, y, x, _whole("W", W, W.shape, (dt,), dev),
-                _whole("bias", bias, torch.Size((rows,)), tuple(_DT), dev), r, z, tokens, rows, cols,
+                _whole("bias", bias, torch.Size((rows,)), _TYPES, dev), r, z, tokens, rows, cols,
                 ctypes.byref(opt))
 
 
@@ -614,8 +620,8 @@ def dion2_linear_backward_weight(G, dY, X, *, dbias=None, accumulate=False, work
     dy, opt.ld_dy = _rows("dY", dY, dY.shape, dt, dev)
     x, opt.ld_x = _rows("X", X, torch.Size((tokens, cols)), dt, dev)
     _layer_call(load().dion2_linear_backward_weight, dev, stream,
-                _whole("G", G, torch.Size((rows, cols)), tuple(_DT), dev),
-                _whole("dbias", dbias, torch.Size((rows,)), tuple(_DT), dev), dy, x, tokens, rows, cols,
+                _whole("G", G, torch.Size((rows, cols)), _TYPES, dev),
+                _whole("dbias", dbias, torch.Size((rows,)), _TYPES, dev), dy, x, tokens, rows, cols,
                 ctypes.byref(opt))
 
 
@@ -645,7 +651,7 @@ def dion2_layernorm_forward(Y, X, gamma=None, beta=None, *, eps=1e-5, mean=None,
     _layer_call(load().dion2_layernorm_forward, dev, stream, y,
                 _whole("mean", mean, stat, (torch.float32,), dev),
                 _whole("rstd", rstd, stat, (torch.float32,), dev), x,
-                _whole("gamma", gamma, line, tuple(_DT), dev), _whole("beta", beta, line, tuple(_DT), dev),
+                _whole("gamma", gamma, line, _TYPES, dev), _whole("beta", beta, line, _TYPES, dev),
                 shape[0], shape[1], ctypes.byref(opt))
 
 
@@ -665,10 +671,10 @@ def dion2_layernorm_backward(dX, dY, X, mean, rstd, *, gamma=None, residual_grad
     dr, opt.ld_dr = _rows("residual_grad", residual_grad, shape, dt, dev)
     line, stat = shape[1:], shape[:1]
     _layer_call(load().dion2_layernorm_backward, dev, stream, dx,
-                _whole("dgamma", dgamma, line, tuple(_DT), dev), _whole("dbeta", dbeta, line, tuple(_DT), dev),
+                _whole("dgamma", dgamma, line, _TYPES, dev), _whole("dbeta", dbeta, line, _TYPES, dev),
                 dy, x, _whole("mean", mean, stat, (torch.float32,), dev),
                 _whole("rstd", rstd, stat, (torch.float32,), dev),
-                _whole("gamma", gamma, line, tuple(_DT), dev), dr, shape[0], shape[1], ctypes.byref(opt))
+                _whole("gamma", gamma, line, _TYPES, dev), dr, shape[0], shape[1], ctypes.byref(opt))
 
 
 def dion2_linear_workspace_size(tokens, rows, cols, dtype=torch.bfloat16) -> int:
