@@ -87,11 +87,14 @@ def product64(a, b):
 
 
 # (tokens, rows, cols): one entry, single tokens, below and above a vector, tile edges, odd and large, an
-# output of 144 partly filled 256 x 256 tiles in each of the three products, and as many tokens as fill one or two of 16
+# output of 144 partly filled 256 x 256 tiles in each of the three products, and as many tokens as fill one or two of 16;
+# then tiles of 128, and products whose K is cut into parts on tiles of 64, 128 and 256
 SIZES = [(1, 1, 1), (1, 96, 64), (1, 257, 1000), (2, 33, 7), (3, 8, 130), (5, 1000, 264), (16, 300, 520), (17, 64, 64),
          (31, 7, 33), (64, 128, 128), (127, 129, 130), (128, 256, 512), (129, 100, 8), (300, 264, 257), (515, 130, 72),
          (1024, 520, 2048), (700, 1000, 517), (2900, 2824, 200), (2900, 72, 2824), (72, 2904, 2824),
-         (16, 1000, 4104), (32, 520, 2048), (33, 264, 264)]
+         (16, 1000, 4104), (32, 520, 2048), (33, 264, 264),
+         (2200, 2056, 136), (2200, 136, 2056), (136, 2200, 2056), (72, 520, 8200), (72, 8200, 520), (8200, 72, 520),
+         (2048, 2048, 8192), (3000, 2048, 8192), (8192, 3000, 2048)]
 ACTS = sorted(ACTIVATIONS)
 
 
@@ -328,6 +331,15 @@ def test_layernorm_backward(hip_device, i, dtype):
     binding.dion2_layernorm_backward(None, dY, X, mean, rstd, gamma=gamma, dgamma=a, accumulate=add)
     binding.dion2_layernorm_backward(None, dY, X, mean, rstd, gamma=gamma, dbeta=b, accumulate=add)
     assert torch.equal(a, dg.view[0]) and torch.equal(b, db.view[0])
+    if dR is not None:
+        keep = dR.clone()
+        binding.dion2_layernorm_backward(dR, dY, X, mean, rstd, gamma=gamma, residual_grad=dR, dgamma=a, dbeta=b)
+        assert torch.equal(dR, dX.view)
+        dR.copy_(keep)
+    x0, a0, b0 = X.clone(), dg0.clone(), db0.clone()
+    binding.dion2_layernorm_backward(X, dY, X, mean, rstd, gamma=gamma, residual_grad=dR, dgamma=a0, dbeta=b0, accumulate=add)
+    assert torch.equal(X, dX.view) and torch.equal(a0, dg.view[0]) and torch.equal(b0, db.view[0])
+    X.copy_(x0)
     binding.dion2_layernorm_backward(dY, dY, X, mean, rstd, gamma=gamma, residual_grad=dR, dgamma=a, dbeta=b)
     assert torch.equal(dY, dX.view)
 
@@ -536,6 +548,54 @@ def test_rows_past_2_31_entries(hip_device):
     binding.dion2_linear_backward_weight(G, dY, X)
     want, _ = product64(dY[-300:].t(), X[-300:].t())
     near(G, want, (t + 16) * 2.0 ** -23 * (dY[-300:].double().abs().t() @ X[-300:].double().abs()), F32, "G")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_long_pitches(hip_device, dtype):
+    """Rows 2^21 + 8 entries apart: more than the directly fed tiles address."""
+    g = gen_of("pitch", dtype == BF)
+    t, r, c, pitch = 70, 72, 136, (1 << 21) + 8
+    buf = torch.zeros((t, pitch), dtype=dtype, device="cuda")
+    X, dY = buf[:, :c], buf[:, c:c + r]
+    X.copy_(rnd((t, c), dtype, g))
+    dY.copy_(rnd((t, r), dtype, g))
+    W, Y, G = rnd((r, c), dtype, g, 0.1), buf[:, 1024:1024 + r], torch.empty((r, c), dtype=F32, device="cuda")
+    binding.dion2_linear_forward(Y, X, W)
+    near(Y, *product64(X, W), dtype, "Y")
+    binding.dion2_linear_backward_weight(G, dY, X)
+    near(G, *product64(dY.t(), X.t()), F32, "G")
+    dX = buf[:, 2048:2048 + c]
+    binding.dion2_linear_backward_input(dX, dY, W)
+    near(dX, *product64(dY, W.t()), dtype, "dX")
+
+
+def test_threads_share_a_stream(hip_device):
+    """Two host threads, two calls each in turn, on one stream and the library's workspace: the calls take turns."""
+    import threading
+    jobs = [every_call(300, 136, 264, BF, s) for s in (5, 6)]
+    for run, _ in jobs:
+        run()
+    torch.cuda.synchronize()
+    want = [{k: v.clone() for k, v in o.items()} for _, o in jobs]
+    fails = []
+
+    def work(run, o, w):
+        try:
+            for _ in range(20):
+                run()
+        except Exception as e:   # noqa: BLE001 - reported by the test
+            fails.append(e)
+
+    threads = [threading.Thread(target=work, args=(run, o, w)) for (run, o), w in zip(jobs, want)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    torch.cuda.synchronize()
+    assert not fails
+    for (_, o), w in zip(jobs, want):
+        for k in o:
+            assert torch.equal(o[k], w[k]), k
 
 
 def test_more_rows_than_a_launch_has_blocks(hip_device):
