@@ -1,5 +1,6 @@
 /*
- * dion2.h -- C ABI of the Dion2 optimizer step for AMD Instinct MI355X (gfx950).
+ * dion2.h -- C ABI of the Dion2 optimizer step for AMD Instinct MI355X (gfx950),
+ * and of the layers around it ("The layers around the step" below).
  *
  * The step is Algorithm 1 of "Dion2: A Simple Method to Shrink Matrix in
  * Muon" (Ahn, Amsel, Langford), applied to every matrix of a batch of

@@ -968,8 +968,8 @@ int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return ((M + bm - 1) / 
 //   1024 x 1024, K 1024:  64 6.2, 128 12.0 us;  1024 x 2048:  8.6, 12.4
 //   2048 x 4096, K 1024:  64 30, 128 21.8, 256 28.6
 //   2048 x 8192, K 2048:  64 107, 128 69, 256 58.7
-// A product cut into parts adds their round trip through memory at 4 TB/s and
-// a launch: 2048 x 2048, K 8192 on 128 x 128 tiles 86.6 whole, 73.3 in two;
+// A product cut into parts adds their round trip through the caches at 8 TB/s
+// and a launch: 2048 x 2048, K 8192 on 128 x 128 tiles 86.6 whole, 73.3 in two;
 // 64 x 2048, K 8192 on 64 x 64 tiles 28 whole, 13.2 in eight.
 struct Cost {
     int tile, most;
@@ -987,7 +987,7 @@ double time_of(const Cost& c, const ProductArgs& a, int splits) {
     const int64_t rounds = tiles / (256 * c.most), left = (tiles % (256 * c.most) + 255) / 256;
     double t = rounds * (c.fixed + units * c.unit[c.most - 1]);
     if (left) t += c.fixed + units * c.unit[left - 1];
-    if (splits > 1) t += 3.0 + (double)splits * a.M * a.N * 8 / 4e6;
+    if (splits > 1) t += 3.0 + (double)splits * a.M * a.N * 8 / 8e6;
     return t;
 }
 
