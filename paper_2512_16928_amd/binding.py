@@ -677,9 +677,10 @@ def dion2_layernorm_backward(dX, dY, X, mean, rstd, *, gamma=None, residual_grad
                 _whole("gamma", gamma, line, _TYPES, dev), dr, shape[0], shape[1], ctypes.byref(opt))
 
 
-def dion2_linear_workspace_size(tokens, rows, cols, dtype=torch.bfloat16) -> int:
-    """Workspace bytes that suffice for every linear call of these sizes (0: none needed)."""
-    opt = LayerOptions(dtype=_DT[dtype], p_dtype=DTYPE_BF16, g_dtype=DTYPE_BF16)
+def dion2_linear_workspace_size(tokens, rows, cols, dtype=torch.bfloat16, *, ld_x=0, ld_dy=0) -> int:
+    """Workspace bytes that suffice for every linear call of these sizes (0: none needed), with rows
+    of X ld_x and of dY ld_dy entries apart (0: contiguous)."""
+    opt = LayerOptions(dtype=_DT[dtype], p_dtype=DTYPE_BF16, g_dtype=DTYPE_BF16, ld_x=ld_x, ld_dy=ld_dy)
     return int(load().dion2_linear_workspace_size(tokens, rows, cols, ctypes.byref(opt)))
 
 

@@ -321,7 +321,8 @@ __global__ __launch_bounds__(kGThreads) void product_any(ProductArgs a) {
 }
 
 // -------------------------------------------------- bf16 tiles, LDS fed directly
-// For operands whose rows start on 16-byte boundaries. K-slices go from
+// For operands whose rows start on 16-byte boundaries and are whole chunks of 16
+// bytes long (others are copied so first, with zeros behind). K-slices go from
 // global memory straight into LDS (16 bytes a lane, a wave's 1 KB a time), S
 // slices in flight, through buffer descriptors: a lane whose chunk lies past
 // an edge asks for an offset past the descriptor's range and gets zeros.
@@ -355,6 +356,10 @@ __device__ __forceinline__ void wait_vmcnt() {
     __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4)); }
+
+// Rows of an operand: an m/n-contiguous one has them in whole chunks.
+template <bool KMAJOR>
+__device__ __forceinline__ int64_t extent(int64_t rows) { return KMAJOR ? rows : (rows + 7) & ~(int64_t)7; }
 
 // One operand of a tile: R rows (m or n), slices of BK. HALF 0, 1: every first,
 // second run of 64 rows of a tile of 2 R (what a wave of a 256-row tile reads
@@ -661,8 +666,8 @@ __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
     const int64_t k_end = s1 == slices ? a.K : (int64_t)s1 * T::BK;
     OA oa;
     OB ob;
-    oa.init(static_cast<const uint16_t*>(a.A) + (AK ? m0 * a.lda + k0 : k0 * a.lda + m0), a.lda, a.M - m0, k_end - k0, wave, lane);
-    ob.init(static_cast<const uint16_t*>(a.B) + (BKM ? n0 * a.ldb + k0 : k0 * a.ldb + n0), a.ldb, a.N - n0, k_end - k0, wave, lane);
+    oa.init(static_cast<const uint16_t*>(a.A) + (AK ? m0 * a.lda + k0 : k0 * a.lda + m0), a.lda, extent<AK>(a.M) - m0, k_end - k0, wave, lane);
+    ob.init(static_cast<const uint16_t*>(a.B) + (BKM ? n0 * a.ldb + k0 : k0 * a.ldb + n0), a.ldb, extent<BKM>(a.N) - n0, k_end - k0, wave, lane);
     auto request = [&](unsigned char* st) {
 #pragma unroll
         for (int q = 0; q < OA::Q; ++q) oa.load(q, st, wave);
@@ -761,9 +766,9 @@ __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a
     O0 o0;
     O1 o1;
     OB ob;
-    o0.init(A, a.lda, a.M - m0, k, wave, lane);
-    o1.init(A, a.lda, a.M - m0, k, wave, lane);
-    ob.init(B, a.ldb, a.N - n0, k, wave, lane);
+    o0.init(A, a.lda, extent<AK>(a.M) - m0, k, wave, lane);
+    o1.init(A, a.lda, extent<AK>(a.M) - m0, k, wave, lane);
+    ob.init(B, a.ldb, extent<BKM>(a.N) - n0, k, wave, lane);
     // a stage: A's first half, its second, B
     auto request_first = [&](unsigned char* st) {
 #pragma unroll
@@ -912,6 +917,23 @@ __global__ __launch_bounds__(64 * WAVES) void product_few(ProductArgs a) {
     });
 }
 
+// Copies of operands in whole chunks of 16 bytes, zeros behind each row: a chunk
+// a thread; blockIdx.y is the operand.
+struct CopyArgs {
+    const uint16_t* from[2];
+    uint16_t* to[2];
+    int64_t ld[2], rows[2], width[2];
+};
+__global__ __launch_bounds__(256) void copy_chunks(CopyArgs a) {
+    const int o = blockIdx.y;
+    const int64_t chunks = (a.width[o] + 7) / 8, total = a.rows[o] * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / chunks, c = i % chunks * 8;
+        const int n = a.width[o] - c < 8 ? (int)(a.width[o] - c) : 8;
+        stg(a.to[o] + 8 * i, load_chunk(a.from[o] + r * a.ld[o] + c, n, c));
+    }
+}
+
 // Adds the parts of a split product in order and finishes its entries: one
 // wave a 32 x 32 block.
 template <Product KIND, typename T>
@@ -945,17 +967,27 @@ enum Form { FORM_ANY, FORM_ANY_64, FORM_FEW, FORM_SMALL, FORM_MIDDLE, FORM_BIG }
 struct Plan {
     Form form;
     int splits;
+    bool copy_a, copy_b;   // the operand is copied in whole chunks first
 };
 
-// The operands can be read in whole aligned chunks of 16 bytes.
-bool whole_chunks(Product kind, const ProductArgs& a) {
-    auto aligned = [](const void* p, int64_t ld) {
-        return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && ld < (int64_t(1) << 21);
-    };
-    const bool inner = kind == PROD_FORWARD ? a.K % 8 == 0
-                       : kind == PROD_INPUT ? a.K % 8 == 0 && a.N % 8 == 0
-                                            : a.M % 8 == 0 && a.N % 8 == 0;
-    return a.bf16 && inner && aligned(a.A, a.lda) && aligned(a.B, a.ldb);
+// An operand as it is stored: outer rows of inner entries.
+struct Stored {
+    const void* p;
+    int64_t ld, outer, inner;
+    // Rows are whole chunks of 16 bytes from one 16-byte boundary to the next.
+    // Sizes and pitches alone say whether a copy is needed, so that the
+    // workspace can be told in advance; of the others the pointer must be aligned.
+    bool whole() const { return ld % 8 == 0 && inner % 8 == 0 && ld < (int64_t(1) << 21); }
+    bool aligned() const { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+    size_t copy_bytes() const { return ((size_t)outer * ((inner + 7) / 8 * 16) + 255) & ~size_t(255); }
+};
+Stored stored_a(Product kind, const ProductArgs& a) {
+    if (kind == PROD_WEIGHT) return {a.A, a.lda, a.K, a.M};
+    return {a.A, a.lda, a.M, a.K};
+}
+Stored stored_b(Product kind, const ProductArgs& a) {
+    if (kind == PROD_FORWARD) return {a.B, a.ldb, a.N, a.K};
+    return {a.B, a.ldb, a.K, a.N};
 }
 
 int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
@@ -981,9 +1013,9 @@ constexpr Cost kBigCost = {256, 1, 10.0, {1.5}};
 constexpr Cost kAny64Cost[2] = {{64, 4, 2.7, {2.3, 3.2, 4.3, 5.5}}, {64, 4, 2.7, {0.6, 0.9, 1.05, 1.2}}};   // fp32, bf16
 constexpr Cost kAnyCost[2] = {{128, 2, 4.0, {6.1, 10.4}}, {128, 2, 4.0, {1.5, 2.0}}};
 
-double time_of(const Cost& c, const ProductArgs& a, int splits) {
+double time_of(const Cost& c, const ProductArgs& a, int splits, double slow) {
     const int64_t tiles = tiles_of(a.M, a.N, c.tile, c.tile) * splits;
-    const double units = (double)((a.K + 63) / 64) / splits;
+    const double units = slow * (double)((a.K + 63) / 64) / splits;
     const int64_t rounds = tiles / (256 * c.most), left = (tiles % (256 * c.most) + 255) / 256;
     double t = rounds * (c.fixed + units * c.unit[c.most - 1]);
     if (left) t += c.fixed + units * c.unit[left - 1];
@@ -991,27 +1023,42 @@ double time_of(const Cost& c, const ProductArgs& a, int splits) {
     return t;
 }
 
+// Copies cost a launch and their bytes at 4 TB/s. Forward, input and weight
+// gradient of 8191 tokens through 2047 x 2041: 78, 75 and 103 us with copies, on
+// tiles of any alignment 144, 202 and 284; 1531 tokens through 1000 x 517: 12.5,
+// 10.6, 13.3 and 10.3, 18.7, 16.4.
 Plan plan_of(Product kind, const ProductArgs& a) {
-    Plan best{FORM_FEW, 1};
-    const bool whole = whole_chunks(kind, a);
-    if (whole && kind == PROD_FORWARD && a.M <= 32) return best;
+    Plan best{FORM_FEW, 1, false, false};
+    const Stored sa = stored_a(kind, a), sb = stored_b(kind, a);
+    const bool copy_a = !sa.whole(), copy_b = !sb.whole();
+    const bool direct = a.bf16 && (copy_a || sa.aligned()) && (copy_b || sb.aligned());
+    if (direct && !copy_a && !copy_b && kind == PROD_FORWARD && a.M <= 32) return best;
     double least = 0.0;
-    auto offer = [&](Form form, const Cost& c) {
+    // slow: of the units; more: us once
+    auto offer = [&](Form form, const Cost& c, double slow, double more, bool ca, bool cb) {
         for (int splits = 1; splits <= 32 && (splits == 1 || (a.K + 63) / 64 >= splits); splits *= 2) {
-            const double t = time_of(c, a, splits);
+            const double t = time_of(c, a, splits, slow) + more;
             if (best.form == FORM_FEW || t < least) {
-                best = {form, splits};
+                best = {form, splits, ca, cb};
                 least = t;
             }
         }
     };
-    if (whole) {
-        offer(FORM_BIG, kBigCost);
-        offer(FORM_MIDDLE, kMiddleCost);
-        offer(FORM_SMALL, kSmallCost);
-    } else {
-        offer(FORM_ANY, kAnyCost[a.bf16]);
-        offer(FORM_ANY_64, kAny64Cost[a.bf16]);
+    if (direct) {
+        const double bytes = (copy_a ? 4.0 * sa.outer * sa.inner : 0.0) + (copy_b ? 4.0 * sb.outer * sb.inner : 0.0);
+        const double more = copy_a || copy_b ? 5.0 + bytes / 4e6 : 0.0;
+        offer(FORM_BIG, kBigCost, 1.0, more, copy_a, copy_b);
+        offer(FORM_MIDDLE, kMiddleCost, 1.0, more, copy_a, copy_b);
+        offer(FORM_SMALL, kSmallCost, 1.0, more, copy_a, copy_b);
+    }
+    if (!direct || copy_a || copy_b) {
+        // rows of odd width read across: 1.1 to 2.2 times a unit's time, by 1.4 for
+        // each m/n-contiguous operand
+        double slow = 1.0;
+        if (a.bf16 && copy_a && kind == PROD_WEIGHT) slow *= 1.4;
+        if (a.bf16 && copy_b && kind != PROD_FORWARD) slow *= 1.4;
+        offer(FORM_ANY, kAnyCost[a.bf16], slow, 0.0, false, false);
+        offer(FORM_ANY_64, kAny64Cost[a.bf16], slow, 0.0, false, false);
     }
     return best;
 }
@@ -1063,13 +1110,43 @@ hipError_t launch_type(const ProductArgs& a, Form form, hipStream_t s) {
     return a.bf16 ? launch_kind<KIND, uint16_t>(a, form, s) : launch_kind<KIND, float>(a, form, s);
 }
 
-size_t part_bytes(const ProductArgs& a, int splits) {
-    return splits > 1 ? (size_t)splits * tiles_of(a.M, a.N, 32, 32) * 4096 : 0;
+size_t copy_bytes(Product kind, const ProductArgs& a, const Plan& p) {
+    return (p.copy_a ? stored_a(kind, a).copy_bytes() : 0) + (p.copy_b ? stored_b(kind, a).copy_bytes() : 0);
+}
+
+// The copies that the plan asks for, at the workspace's start; the product then
+// reads them, and its parts follow.
+hipError_t make_copies(Product kind, ProductArgs& a, const Plan& p, hipStream_t s) {
+    CopyArgs c{};
+    int n = 0;
+    char* to = reinterpret_cast<char*>(a.part);
+    int64_t chunks = 0;
+    auto add = [&](const Stored& o, const void** pointer, int64_t* ld) {
+        c.from[n] = static_cast<const uint16_t*>(o.p);
+        c.to[n] = reinterpret_cast<uint16_t*>(to);
+        c.ld[n] = o.ld; c.rows[n] = o.outer; c.width[n] = o.inner;
+        chunks = std::max(chunks, o.outer * ((o.inner + 7) / 8));
+        *pointer = to;
+        *ld = (o.inner + 7) / 8 * 8;
+        to += o.copy_bytes();
+        ++n;
+    };
+    if (p.copy_a) add(stored_a(kind, a), &a.A, &a.lda);
+    if (p.copy_b) add(stored_b(kind, a), &a.B, &a.ldb);
+    a.part = reinterpret_cast<float*>(to);
+    if (!n || !chunks) return hipSuccess;
+    copy_chunks<<<dim3((unsigned)std::min<int64_t>((chunks + 255) / 256, 8192), (unsigned)n), 256, 0, s>>>(c);
+    return hipGetLastError();
+}
+
+size_t plan_bytes(Product kind, const ProductArgs& a, const Plan& p) {
+    const size_t parts = p.splits > 1 ? (size_t)p.splits * tiles_of(a.M, a.N, 32, 32) * 4096 : 0;
+    return copy_bytes(kind, a, p) + parts;
 }
 
 }  // namespace
 
-size_t product_workspace(Product kind, const ProductArgs& a) { return part_bytes(a, plan_of(kind, a).splits); }
+size_t product_workspace(Product kind, const ProductArgs& a) { return plan_bytes(kind, a, plan_of(kind, a)); }
 
 int64_t product_row_sums(const ProductArgs& a) {
     const Plan p = plan_of(PROD_WEIGHT, a);
@@ -1078,21 +1155,23 @@ int64_t product_row_sums(const ProductArgs& a) {
     return tile ? (int64_t)p.splits * waves * ((a.N + tile - 1) / tile) : 0;
 }
 
-size_t product_workspace_most(Product kind, int64_t M, int64_t N, int64_t K, int bf16) {
-    // the most over what pointers and pitches can make of it: chunks whole or not
-    ProductArgs a{};
-    a.M = M; a.N = N; a.K = K; a.bf16 = bf16;
-    a.lda = a.ldb = 8;
-    const size_t sums = kind == PROD_WEIGHT ? (size_t)product_row_sums(a) * M * 4 : 0;
-    const size_t whole = product_workspace(kind, a) + sums;
-    a.lda = 1;
-    return std::max(whole, product_workspace(kind, a));
+size_t product_workspace_most(Product kind, ProductArgs a) {
+    // the most over what the pointers can be: aligned or not
+    size_t most = 0;
+    for (uintptr_t at : {(uintptr_t)0, (uintptr_t)2}) {
+        a.A = a.B = reinterpret_cast<const void*>(at);
+        const size_t sums = kind == PROD_WEIGHT ? (size_t)product_row_sums(a) * a.M * 4 : 0;
+        most = std::max(most, product_workspace(kind, a) + sums);
+    }
+    return most;
 }
 
 hipError_t launch_product(Product kind, ProductArgs a, hipStream_t s) {
     if (a.M == 0 || a.N == 0) return hipSuccess;
     const Plan p = plan_of(kind, a);
     a.splits = p.splits;
+    hipError_t e = make_copies(kind, a, p, s);
+    if (e != hipSuccess) return e;
     if (kind == PROD_FORWARD) return launch_type<PROD_FORWARD>(a, p.form, s);
     if (kind == PROD_INPUT) return launch_type<PROD_INPUT>(a, p.form, s);
     return launch_type<PROD_WEIGHT>(a, p.form, s);

@@ -193,7 +193,7 @@ struct ProductArgs {
     int bias_bf16;
     int out_bf16;       // type of PROD_WEIGHT's out
     int accumulate;
-    float* part;        // partial sums: product_workspace bytes
+    float* part;        // product_workspace bytes, 256-byte aligned: copies, partial sums
     int splits;         // set by launch_product
     float* row_sums;    // nullable, PROD_WEIGHT: [product_row_sums(a)][M], partial sums
                         // over k of A's rows (the bias gradient's)
@@ -201,9 +201,9 @@ struct ProductArgs {
 // How many rows of row_sums PROD_WEIGHT gives; 0 where its form gives none.
 int64_t product_row_sums(const ProductArgs& a);
 // Bytes of workspace of this call without row_sums, and the most of any call of
-// these sizes, with them.
+// these sizes and pitches, with them.
 size_t product_workspace(Product kind, const ProductArgs& a);
-size_t product_workspace_most(Product kind, int64_t M, int64_t N, int64_t K, int bf16);
+size_t product_workspace_most(Product kind, ProductArgs a);
 hipError_t launch_product(Product kind, ProductArgs a, hipStream_t s);
 
 // -------------------------------------------------------- streaming passes

@@ -395,11 +395,16 @@ int dion2_layernorm_backward(void* dX, void* dgamma, void* dbeta, const void* dY
 size_t dion2_linear_workspace_size(int64_t tokens, int64_t rows, int64_t cols, const dion2_layer_options* opt) {
     const dion2_layer_options o = options_of(opt);
     if (check_options(o) != DION2_OK || check_sizes(tokens, rows, cols) != DION2_OK) return 0;
-    const int bf16 = o.dtype == DION2_DTYPE_BF16;
-    const size_t weight = align256(product_workspace_most(PROD_WEIGHT, rows, cols, tokens, bf16)) +
-                          align256((size_t)col_sum_blocks(tokens, rows) * rows * 4);
-    return std::max({align256(product_workspace_most(PROD_FORWARD, tokens, rows, cols, bf16)),
-                     align256(product_workspace_most(PROD_INPUT, tokens, cols, rows, bf16)), weight});
+    ProductArgs f{}, i{}, w{};
+    f.bf16 = i.bf16 = w.bf16 = o.dtype == DION2_DTYPE_BF16;
+    f.lda = w.ldb = pitch(o.ld_x, cols);
+    i.lda = w.lda = pitch(o.ld_dy, rows);
+    f.ldb = i.ldb = cols;
+    f.M = tokens; f.N = rows; f.K = cols;
+    i.M = tokens; i.N = cols; i.K = rows;
+    w.M = rows; w.N = cols; w.K = tokens;
+    return std::max({align256(product_workspace_most(PROD_FORWARD, f)), align256(product_workspace_most(PROD_INPUT, i)),
+                     align256(product_workspace_most(PROD_WEIGHT, w)) + align256((size_t)col_sum_blocks(tokens, rows) * rows * 4)});
 }
 
 size_t dion2_layernorm_workspace_size(int64_t tokens, int64_t cols, const dion2_layer_options* opt) {

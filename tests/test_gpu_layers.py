@@ -569,6 +569,42 @@ def test_long_pitches(hip_device, dtype):
     near(dX, *product64(dY, W.t()), dtype, "dX")
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("t,r,c", [(40, 72, 136), (300, 264, 1032), (2200, 2056, 136), (2200, 136, 2056)])
+def test_pointers_between_vectors(hip_device, t, r, c, dtype):
+    """Whole widths and pitches, but activations that start one entry past a 16-byte boundary."""
+    g = gen_of("between", t, r, c, dtype == BF)
+    X = Framed(t, c, dtype, 1, 8, rnd((t, c), dtype, g)).view
+    dY = Framed(t, r, dtype, 1, 8, rnd((t, r), dtype, g, 1e-2)).view
+    W, Y, dX = rnd((r, c), dtype, g, 0.1), Framed(t, r, dtype, 1, 8), Framed(t, c, dtype, 1, 8)
+    G, db = torch.empty((r, c), dtype=F32, device="cuda"), torch.empty(r, dtype=F32, device="cuda")
+    binding.dion2_linear_forward(Y.view, X, W)
+    near(Y.view, *product64(X, W), dtype, "Y")
+    binding.dion2_linear_backward_input(dX.view, dY, W)
+    near(dX.view, *product64(dY, W.t()), dtype, "dX")
+    binding.dion2_linear_backward_weight(G, dY, X, dbias=db)
+    near(G, *product64(dY.t(), X.t()), F32, "G")
+    near(db, dY.double().sum(0), (t + 16) * 2.0 ** -23 * dY.double().abs().sum(0), F32, "dbias")
+    assert Y.intact() and dX.intact()
+
+
+@pytest.mark.parametrize("t,r,c", [(300, 131, 517), (1100, 519, 263), (2500, 2051, 77), (3000, 131, 2055), (5, 1003, 2051)])
+def test_odd_widths_with_the_callers_workspace(hip_device, t, r, c):
+    """Widths that are no multiple of 8: operands are copied into the workspace, whose stated size is enough and whose
+    content does not matter; without it the results are the same."""
+    run, o = every_call(t, r, c, BF, 3)
+    run()
+    first = {k: v.clone() for k, v in o.items()}
+    need = max(binding.dion2_linear_workspace_size(t, r, c), binding.dion2_layernorm_workspace_size(t, c))
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    run2, o2 = every_call(t, r, c, BF, 3, workspace=ws[:need])
+    run2()
+    torch.cuda.synchronize()
+    for k in first:
+        assert torch.equal(first[k], o2[k]), k
+    assert bool((ws[need:] == 0xFF).all())
+
+
 def test_threads_share_a_stream(hip_device):
     """Two host threads, two calls each in turn, on one stream and the library's workspace: the calls take turns."""
     import threading
