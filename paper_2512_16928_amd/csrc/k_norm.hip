@@ -31,6 +31,13 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
     return s;
 }
 
+// From the mean square deviation about a rounded mean and that mean's error,
+// which rounding can leave a little below 0 (a NaN stays one).
+__device__ __forceinline__ float variance(float d2, float off) {
+    const float v = d2 - off * off;
+    return v < 0.0f ? 0.0f : v;
+}
+
 __device__ __forceinline__ int part8(int64_t n, int64_t at) { return n - at < 8 ? (int)(n - at) : 8; }
 
 // ---- rows held in registers
@@ -185,7 +192,7 @@ __global__ __launch_bounds__(64 * row_waves(WPR)) void norm_regs(NormArgs a) {
     }
     row_sums<WPR>(d1, d2, red, turn);
     const float off = d1 * inv;
-    const float rstd = 1.0f / sqrtf(d2 * inv - off * off + a.eps);
+    const float rstd = 1.0f / sqrtf(variance(d2 * inv, off) + a.eps);
     T* y = static_cast<T*>(a.Y) + t * a.ldy;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
@@ -378,7 +385,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows(NormArgs a) {
             }
         }
         const float off = block_sum(d1, red) / n;
-        const float rstd = 1.0f / sqrtf(block_sum(d2, red) / n - off * off + a.eps);
+        const float rstd = 1.0f / sqrtf(variance(block_sum(d2, red) / n, off) + a.eps);
         for (int64_t c = threadIdx.x * 8; c < a.cols; c += kThreads * 8) {
             const int k = part8(a.cols, c);
             float g[8];

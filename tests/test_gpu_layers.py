@@ -605,6 +605,37 @@ def test_odd_widths_with_the_callers_workspace(hip_device, t, r, c):
     assert bool((ws[need:] == 0xFF).all())
 
 
+@pytest.mark.parametrize("cols", [5, 264, 2041, 5123])
+@pytest.mark.parametrize("t", [1, 7, 16, 17, 32])
+def test_few_tokens_of_any_width(hip_device, t, cols):
+    """Up to 32 tokens take one form, whatever the width, the pitch and the alignment; no entry beside a row is read
+    into it."""
+    g = gen_of("few", t, cols)
+    rows = 203
+    W, bias = rnd((rows, cols), BF, g, 1.0 / math.sqrt(cols)), rnd((rows,), BF, g)
+    for lead, pad in ((0, 0), (1, 3), (0, (1 << 21) + 8)):
+        X, Y = Framed(t, cols, BF, lead, pad, rnd((t, cols), BF, g)), Framed(t, rows, BF, lead, pad % 64)
+        X.buf[~X.used] = float("nan")
+        binding.dion2_linear_forward(Y.view, X.view, W, bias=bias)
+        want, bound = product64(X.view, W)
+        near(Y.view, want + bias.double(), bound + 2.0 ** -22 * (want.abs() + bias.double().abs()), BF, (lead, pad))
+        assert Y.intact()
+
+
+@pytest.mark.parametrize("cols", [9, 1000, 2041, 5000, 20000])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_layernorm_of_large_constant_rows(hip_device, dtype, cols):
+    """The variance of a constant row is 0 and what rounding makes of it is not below. The mean is off by at most
+    (cols + 2) 2^-24 of it, the correction by as much of that, and rstd is at most 1 / sqrt(eps)."""
+    value = torch.tensor([1.0, 1e6 / 3, -1e8 / 3, 1e9 / 7, 3.3e12], device="cuda").to(dtype)
+    X = value[:, None].repeat(1, cols)
+    Y, rstd = torch.empty_like(X), torch.empty(5, device="cuda")
+    binding.dion2_layernorm_forward(Y, X, eps=EPS, rstd=rstd)
+    assert bool(torch.isfinite(rstd).all()) and bool((rstd > 0).all()) and bool((rstd <= EPS ** -0.5 * (1 + 2.0 ** -20)).all())
+    lim = ((cols + 2) * 2.0 ** -24) ** 2 * value.double().abs() * EPS ** -0.5 * (1 + 2.0 ** -6)
+    assert bool((Y.double().abs() <= lim[:, None]).all())
+
+
 def test_threads_share_a_stream(hip_device):
     """Two host threads, two calls each in turn, on one stream and the library's workspace: the calls take turns."""
     import threading
