@@ -437,7 +437,7 @@ int dion2_plan_form(int batch, int64_t rows, int64_t cols, float alpha,
  * dion2_layernorm_workspace_size) then needs the caller's, since a graph
  * may be replayed while the library's is in use or has been moved:
  * DION2_ERR_WORKSPACE otherwise. Calls that share a caller's workspace must be
- * ordered. */
+ * ordered, and it must not overlap their matrices. */
 typedef enum dion2_act {
     DION2_ACT_NONE = 0,
     DION2_ACT_RELU = 1,       /* max(z, 0); slope 0 at 0                       */
@@ -447,7 +447,8 @@ typedef enum dion2_act {
 } dion2_act;
 
 /* Options of the layer calls. Fill with dion2_layer_options_init; opt == NULL
-   means defaults. A call ignores the fields it does not name. */
+   means defaults. Every call checks the types, act and eps; of the others it
+   ignores the fields it does not name. */
 typedef struct dion2_layer_options {
     int dtype;               /* W and all activations (default DION2_DTYPE_BF16)  */
     int p_dtype;             /* bias, gamma, beta (default DION2_DTYPE_BF16)      */
@@ -520,7 +521,7 @@ int dion2_layernorm_backward(void* dX, void* dgamma, void* dbeta, const void* dY
    where none is needed or the sizes or types are invalid. Linear calls use it
    for parts of a sum over few output tiles, and for copies of bf16 operands
    whose width or pitch is no multiple of 8 (which then run at the speed of
-   those whose is). */
+   those whose is), 2 GiB of copies at most. */
 size_t dion2_linear_workspace_size(int64_t tokens, int64_t rows, int64_t cols,
                                    const dion2_layer_options* opt);
 size_t dion2_layernorm_workspace_size(int64_t tokens, int64_t cols,

@@ -5,7 +5,8 @@
 // Sums are fp32 (the MFMA accumulators); a result is rounded once, at its
 // store. Where a launch has too few tiles for the chip, K is cut into parts:
 // their fp32 sums go to the workspace and a second launch adds them in order
-// and finishes the entries, so results depend on the sizes alone.
+// and finishes the entries, so results depend on the sizes, pitches and
+// alignment alone.
 #include <algorithm>
 #include <type_traits>
 
@@ -860,8 +861,9 @@ __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a
 // ----------------------------------------------------------- few tokens
 // Y for at most 32 tokens (an answering model's steps): W's rows are the work,
 // read once, straight into MFMA fragments (16 x 16 x 32: a lane has 8
-// consecutive k of one of 16 rows, so an instruction reads 64-byte pieces); a
-// block's waves share 16 rows, each a run of k, and add up in LDS.
+// consecutive k of one of 16 rows, so an instruction reads 64-byte pieces, from
+// any element boundary); a block's waves share 16 rows, each a run of k, and add
+// up in LDS.
 template <int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void product_few(ProductArgs a) {
     constexpr int U = NT == 1 ? (WAVES == 4 ? 16 : 8) : 4;   // k-steps whose loads are on their way together
@@ -882,13 +884,13 @@ __global__ __launch_bounds__(64 * WAVES) void product_few(ProductArgs a) {
     f32x4 acc[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int K = (int)a.K, steps = (K + 31) / 32;
+    const int K = (int)a.K, whole = K & ~7, steps = (K + 31) / 32;
     const int s1 = steps * (wave + 1) / WAVES;
     for (int s = steps * wave / WAVES; s < s1; s += U) {
         uint4 fw[U], fx[U][NT];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const bool in = s + u < s1 && 32 * (s + u) + kl < K;
+            const bool in = s + u < s1 && 32 * (s + u) + kl < whole;
             fw[u] = in ? ldg<uint4>(w + 32 * (s + u)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
             for (int t = 0; t < NT; ++t) fx[u][t] = in ? ldg<uint4>(x[t] + 32 * (s + u)) : make_uint4(0, 0, 0, 0);
@@ -899,6 +901,16 @@ __global__ __launch_bounds__(64 * WAVES) void product_few(ProductArgs a) {
             for (int t = 0; t < NT; ++t)
                 acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[u]),
                                                                  __builtin_bit_cast(bf16x8, fx[u][t]), acc[t], 0, 0, 0);
+    }
+    if (whole < K && wave == WAVES - 1) {   // the last 1 to 7 of k, as the first lanes' chunk
+        const bool in = lane < 16;
+        const uint4 z = make_uint4(0, 0, 0, 0), f = in ? load_chunk(w + whole, K - whole, whole) : z;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint4 g = in ? load_chunk(x[t] + whole, K - whole, whole) : z;
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, g),
+                                                             acc[t], 0, 0, 0);
+        }
     }
     // lane l has rows 4 (l / 16) + 0 .. 3 of token l mod 16
 #pragma unroll
@@ -1027,12 +1039,15 @@ double time_of(const Cost& c, const ProductArgs& a, int splits, double slow) {
 // gradient of 8191 tokens through 2047 x 2041: 78, 75 and 103 us with copies, on
 // tiles of any alignment 144, 202 and 284; 1531 tokens through 1000 x 517: 12.5,
 // 10.6, 13.3 and 10.3, 18.7, 16.4.
+// Beyond kCopiesMost they would hold more memory than that time is worth.
+constexpr size_t kCopiesMost = size_t(2) << 30;
 Plan plan_of(Product kind, const ProductArgs& a) {
     Plan best{FORM_FEW, 1, false, false};
     const Stored sa = stored_a(kind, a), sb = stored_b(kind, a);
     const bool copy_a = !sa.whole(), copy_b = !sb.whole();
-    const bool direct = a.bf16 && (copy_a || sa.aligned()) && (copy_b || sb.aligned());
-    if (direct && !copy_a && !copy_b && kind == PROD_FORWARD && a.M <= 32) return best;
+    const size_t copied = (copy_a ? sa.copy_bytes() : 0) + (copy_b ? sb.copy_bytes() : 0);
+    const bool direct = a.bf16 && (copy_a || sa.aligned()) && (copy_b || sb.aligned()) && copied <= kCopiesMost;
+    if (a.bf16 && kind == PROD_FORWARD && a.M <= 32) return best;
     double least = 0.0;
     // slow: of the units; more: us once
     auto offer = [&](Form form, const Cost& c, double slow, double more, bool ca, bool cb) {
@@ -1045,8 +1060,7 @@ Plan plan_of(Product kind, const ProductArgs& a) {
         }
     };
     if (direct) {
-        const double bytes = (copy_a ? 4.0 * sa.outer * sa.inner : 0.0) + (copy_b ? 4.0 * sb.outer * sb.inner : 0.0);
-        const double more = copy_a || copy_b ? 5.0 + bytes / 4e6 : 0.0;
+        const double more = copy_a || copy_b ? 5.0 + 2.0 * copied / 4e6 : 0.0;
         offer(FORM_BIG, kBigCost, 1.0, more, copy_a, copy_b);
         offer(FORM_MIDDLE, kMiddleCost, 1.0, more, copy_a, copy_b);
         offer(FORM_SMALL, kSmallCost, 1.0, more, copy_a, copy_b);

@@ -52,6 +52,8 @@ struct Mat {
 };
 
 int64_t pitch(int64_t ld, int64_t width) { return ld ? ld : width; }
+// of a product's operand: a single row's does not matter
+int64_t row_pitch(int64_t rows, int64_t ld, int64_t width) { return rows > 1 ? ld : width; }
 
 int check_mat(const Mat& m) {
     if (!m.p) {
@@ -183,7 +185,7 @@ int linear_forward(void* Y, const void* X, const void* W, const void* bias, cons
                     {"R"});
     if (st != DION2_OK || tokens == 0) return st;
     ProductArgs a{};
-    a.A = X; a.lda = ldx;
+    a.A = X; a.lda = row_pitch(tokens, ldx, cols);
     a.B = W; a.ldb = cols;
     a.M = tokens; a.N = rows; a.K = cols;
     a.out = Y; a.ldo = ldy;
@@ -210,7 +212,7 @@ int linear_backward_input(void* dX, const void* dY, const void* W, const void* Z
                     {"Z"});
     if (st != DION2_OK || tokens == 0) return st;
     ProductArgs a{};
-    a.A = dY; a.lda = lddy;
+    a.A = dY; a.lda = row_pitch(tokens, lddy, rows);
     a.B = W; a.ldb = cols;
     a.M = tokens; a.N = cols; a.K = rows;
     a.out = dX; a.ldo = lddx;
@@ -235,8 +237,8 @@ int linear_backward_weight(void* G, void* dbias, const void* dY, const void* X, 
     c.bf16 = o.dtype == DION2_DTYPE_BF16;
     c.out = dbias; c.out_bf16 = o.g_dtype == DION2_DTYPE_BF16; c.accumulate = o.accumulate != 0;
     ProductArgs a{};
-    a.A = dY; a.lda = lddy;
-    a.B = X; a.ldb = ldx;
+    a.A = dY; a.lda = row_pitch(tokens, lddy, rows);
+    a.B = X; a.ldb = row_pitch(tokens, ldx, cols);
     a.M = rows; a.N = cols; a.K = tokens;
     a.out = G; a.ldo = cols; a.out_bf16 = c.out_bf16;
     a.accumulate = c.accumulate;
@@ -392,25 +394,29 @@ int dion2_layernorm_backward(void* dX, void* dgamma, void* dbeta, const void* dY
     });
 }
 
-size_t dion2_linear_workspace_size(int64_t tokens, int64_t rows, int64_t cols, const dion2_layer_options* opt) {
+size_t dion2_linear_workspace_size(int64_t tokens, int64_t rows, int64_t cols, const dion2_layer_options* opt) try {
     const dion2_layer_options o = options_of(opt);
     if (check_options(o) != DION2_OK || check_sizes(tokens, rows, cols) != DION2_OK) return 0;
     ProductArgs f{}, i{}, w{};
     f.bf16 = i.bf16 = w.bf16 = o.dtype == DION2_DTYPE_BF16;
-    f.lda = w.ldb = pitch(o.ld_x, cols);
-    i.lda = w.lda = pitch(o.ld_dy, rows);
+    f.lda = w.ldb = row_pitch(tokens, pitch(o.ld_x, cols), cols);
+    i.lda = w.lda = row_pitch(tokens, pitch(o.ld_dy, rows), rows);
     f.ldb = i.ldb = cols;
     f.M = tokens; f.N = rows; f.K = cols;
     i.M = tokens; i.N = cols; i.K = rows;
     w.M = rows; w.N = cols; w.K = tokens;
     return std::max({align256(product_workspace_most(PROD_FORWARD, f)), align256(product_workspace_most(PROD_INPUT, i)),
                      align256(product_workspace_most(PROD_WEIGHT, w)) + align256((size_t)col_sum_blocks(tokens, rows) * rows * 4)});
+} catch (const std::exception&) {
+    return 0;
 }
 
-size_t dion2_layernorm_workspace_size(int64_t tokens, int64_t cols, const dion2_layer_options* opt) {
+size_t dion2_layernorm_workspace_size(int64_t tokens, int64_t cols, const dion2_layer_options* opt) try {
     const dion2_layer_options o = options_of(opt);
     if (check_options(o) != DION2_OK || check_sizes(tokens, 1, cols) != DION2_OK) return 0;
     return align256((size_t)norm_grad_blocks(tokens, cols, o.dtype == DION2_DTYPE_BF16) * 2 * cols * 4);
+} catch (const std::exception&) {
+    return 0;
 }
 
 }  // extern "C"

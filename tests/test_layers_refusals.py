@@ -203,3 +203,10 @@ def test_binding_checks_shapes_types_and_strides():
         binding._whole("G", x.to(torch.float16), x.shape, (bf, f32), dev)
     with pytest.raises(ValueError, match="one dtype"):
         binding._one_type("gamma and beta", x, x.float())
+
+
+def test_copies_of_operands_are_bounded(lib):
+    need = [binding.dion2_linear_workspace_size(t, 2047, 2048) for t in (1 << 18, 1 << 21)]
+    assert need[0] >= 1 << 30 and need[1] <= (2 << 30) + (1 << 28)
+    # a single row's pitch and up to 32 tokens' forward pass ask for nothing
+    assert binding.dion2_linear_workspace_size(1, 64, 64, ld_x=1001) == binding.dion2_linear_workspace_size(1, 64, 64)
