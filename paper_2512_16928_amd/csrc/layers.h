@@ -20,9 +20,11 @@ enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SILU
 // (bf16's half step is 2^-8 = 3.9e-3), with fp32 ones of degree 8, 2e-8.
 // Evaluated in fp32 the result is within 1e-6 relative for |x| <= 4 and 4e-6
 // for |x| <= 9 (degree 8; the rounding of x^2 grows through the exponential),
-// 1e-5 (degree 5). e = e^{-x^2 / 2} is returned for the density.
-template <bool FINE>
-__device__ __forceinline__ float normal_cdf(float x, float* e_out) {
+// 1e-5 (degree 5). The value is for -|x|, and with SLOPE that of
+// Phi(x) + x phi(x) for it, which takes no second exponential: either is for
+// x > 0 one less what it is there.
+template <bool FINE, bool SLOPE>
+__device__ __forceinline__ float normal_cdf(float x) {
     const float u = __builtin_fabsf(x);
     const float e = __builtin_amdgcn_exp2f(-0.72134752f * x * x);
     float p;
@@ -47,8 +49,7 @@ __device__ __forceinline__ float normal_cdf(float x, float* e_out) {
         p = __builtin_fmaf(p, t, 0.1869775786f);
         p = __builtin_fmaf(p, t, 0.1831902260f);
     }
-    const float h = p * t * e;
-    *e_out = e;
+    const float h = (SLOPE ? __builtin_fmaf(p, t, -0.39894228f * u) : p * t) * e;
     return x > 0.0f ? 1.0f - h : h;
 }
 
@@ -62,9 +63,8 @@ __device__ __forceinline__ float logistic(float x) {
 // act(z). A NaN stays a NaN.
 template <int ACT, bool FINE>
 __device__ __forceinline__ float act_value(float z) {
-    float e;
     if constexpr (ACT == ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if constexpr (ACT == ACT_GELU) return z * normal_cdf<FINE>(z, &e);
+    if constexpr (ACT == ACT_GELU) return z * normal_cdf<FINE, false>(z);
     // z (1 + tanh v) / 2 = z logistic(2 v), v = sqrt(2 / pi) (z + 0.044715 z^3)
     if constexpr (ACT == ACT_GELU_TANH) return z * logistic<FINE>(z * __builtin_fmaf(0.07135482f, z * z, 1.59576912f));
     if constexpr (ACT == ACT_SILU) return z * logistic<FINE>(z);
@@ -75,14 +75,11 @@ __device__ __forceinline__ float act_value(float z) {
 template <int ACT, bool FINE>
 __device__ __forceinline__ float act_slope(float z) {
     if constexpr (ACT == ACT_RELU) return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
-    if constexpr (ACT == ACT_GELU) {
-        float e;
-        const float c = normal_cdf<FINE>(z, &e);
-        return __builtin_fmaf(z * 0.39894228f, e, c);
-    }
+    if constexpr (ACT == ACT_GELU) return normal_cdf<FINE, true>(z);
     if constexpr (ACT == ACT_GELU_TANH) {
         const float s = logistic<FINE>(z * __builtin_fmaf(0.07135482f, z * z, 1.59576912f));
-        return __builtin_fmaf(z * s * (1.0f - s), __builtin_fmaf(0.21406445f, z * z, 1.59576912f), s);
+        // from |z| = 100 on s (1 - s) is 0, and z^2 must not become infinite beside it
+        return __builtin_fmaf(z * s * (1.0f - s), __builtin_fmaf(0.21406445f, __builtin_fminf(z * z, 1e4f), 1.59576912f), s);
     }
     if constexpr (ACT == ACT_SILU) {
         const float s = logistic<FINE>(z);

@@ -400,6 +400,22 @@ def test_activations_of_infinities_and_nan(hip_device):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_activations_of_large_values(hip_device, act, dtype):
+    """From |z| = 200 on an activation is z or 0 and its slope 1 or 0, also where z^2 and z^3 are past fp32's range."""
+    Z = torch.tensor([[200.0, 1e6, 1e13, 1e18, 3e19, 1e20, 1e30, 3e38]], device="cuda")
+    Z = torch.cat([Z, -Z]).to(dtype)
+    dZ, eye = torch.empty_like(Z), torch.eye(8, device="cuda").to(dtype)
+    binding.dion2_activation_backward(dZ, torch.full_like(Z, 3.0), Z, ACTIVATIONS[act])
+    assert torch.equal(dZ, 3.0 * (Z > 0).to(dtype))
+    Y = torch.empty_like(Z)
+    binding.dion2_linear_forward(Y, Z, eye, act=ACTIVATIONS[act])
+    assert torch.equal(Y, Z.clamp(min=0))
+    binding.dion2_linear_backward_input(dZ, torch.full_like(Z, 3.0), eye, Z=Z, act=ACTIVATIONS[act])
+    assert torch.equal(dZ, 3.0 * (Z > 0).to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_layernorm_rows_of_nan_and_zero_variance(hip_device, dtype):
     X = torch.ones((6, 1000), dtype=dtype, device="cuda")
     X[2, 17] = float("nan")
