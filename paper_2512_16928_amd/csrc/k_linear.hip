@@ -929,6 +929,84 @@ __global__ __launch_bounds__(64 * WAVES) void product_few(ProductArgs a) {
     });
 }
 
+// ------------------------------------------------------- small fp32 products
+// One 32 x 32 tile a block, its waves taking a run of k each and adding up in
+// LDS: products of few tiles in one launch, spread over the chip. Operands come
+// straight into the fragments of v_mfma_f32_32x32x2_f32: a lane holds four
+// consecutive k of its row (16 bytes, or four rows of k), the other half of the
+// wave the next four, and the order of k is the same for both operands.
+template <bool KMAJOR>
+__device__ __forceinline__ uint4 near_chunk(const float* p, int64_t ld, int64_t row, int64_t k, int n) {
+    if constexpr (KMAJOR) {
+        return load_chunk(p + row * ld + k, n, k);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = j < n ? ldg<uint32_t>(p + (k + j) * ld + row) : 0;
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+constexpr int kNearWaves = 4;   // eight: equal; sixteen: 1 us more
+template <Product KIND>
+__global__ __launch_bounds__(64 * kNearWaves) void product_near(ProductArgs a) {
+    constexpr bool AK = KIND != PROD_WEIGHT, BKM = KIND == PROD_FORWARD;
+    constexpr int WAVES = kNearWaves, U = 4;   // steps of eight k whose loads are on their way together (eight: 1 us more)
+    __shared__ float part[WAVES][16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t tiles_n = (a.N + 31) / 32;
+    const int64_t m0 = blockIdx.x / tiles_n * 32, n0 = blockIdx.x % tiles_n * 32;
+    // rows past the edges read the last one; what they give is not stored
+    const int64_t m = m0 + (lane & 31) < a.M ? m0 + (lane & 31) : a.M - 1;
+    const int64_t n = n0 + (lane & 31) < a.N ? n0 + (lane & 31) : a.N - 1;
+    const int kl = 4 * (lane >> 5);
+    const float* A = static_cast<const float*>(a.A);
+    const float* B = static_cast<const float*>(a.B);
+    const int64_t steps = (a.K + 7) / 8, whole = a.K & ~(int64_t)3;
+    const int64_t s1 = steps * (wave + 1) / WAVES;
+    f32x16 acc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+    auto multiply = [&](const uint4& fa, const uint4& fb) {
+        const uint32_t x[4] = {fa.x, fa.y, fa.z, fa.w}, y[4] = {fb.x, fb.y, fb.z, fb.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(y[j]), __uint_as_float(x[j]), acc, 0, 0, 0);
+    };
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    for (int64_t s = steps * wave / WAVES; s < s1; s += U) {
+        uint4 fa[U], fb[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t k = 8 * (s + u) + kl;
+            const bool in = s + u < s1 && k < whole;
+            fa[u] = in ? near_chunk<AK>(A, a.lda, m, k, 4) : zero;
+            fb[u] = in ? near_chunk<BKM>(B, a.ldb, n, k, 4) : zero;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) multiply(fa[u], fb[u]);
+    }
+    if (whole < a.K && wave == WAVES - 1) {   // the last 1 to 3 of k, of the first half
+        const int left = kl ? 0 : (int)(a.K - whole);
+        multiply(left ? near_chunk<AK>(A, a.lda, m, whole, left) : zero, left ? near_chunk<BKM>(B, a.ldb, n, whole, left) : zero);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) part[wave][r][lane] = acc[r];
+    __syncthreads();
+    // lane l of the sums has row l mod 32 and, in registers 4 q .. 4 q + 3,
+    // columns 8 q + 4 (l / 32) + 0 .. 3; a thread finishes eight of a row
+    const int id = threadIdx.x;
+    if (id >= 128) return;
+    const int r = id & 31, q = id >> 5;
+    float v[8] = {};
+#pragma unroll
+    for (int g = 0; g < WAVES; ++g)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += part[g][4 * q + (j & 3)][r + 32 * (j >> 2)];
+    with_act_of<KIND>(a.act, [&](auto act) {
+        finish8_edge<KIND, decltype(act)::value, true, float>(a, m0 + r, n0 + 8 * q, v);
+    });
+}
+
 // Copies of operands in whole chunks of 16 bytes, zeros behind each row: a chunk
 // a thread; blockIdx.y is the operand.
 struct CopyArgs {
@@ -975,7 +1053,7 @@ __global__ __launch_bounds__(64) void product_join(ProductArgs a) {
 typedef Tile<128, 128, 64, 2, 2, 2> MiddleTile;
 typedef Tile<64, 64, 64, 4, 2, 2> SmallTile;
 
-enum Form { FORM_ANY, FORM_ANY_64, FORM_FEW, FORM_SMALL, FORM_MIDDLE, FORM_BIG };
+enum Form { FORM_ANY, FORM_ANY_64, FORM_NEAR, FORM_FEW, FORM_SMALL, FORM_MIDDLE, FORM_BIG };
 struct Plan {
     Form form;
     int splits;
@@ -1015,10 +1093,14 @@ int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return ((M + bm - 1) / 
 // A product cut into parts adds their round trip through the caches at 8 TB/s
 // and a launch: 2048 x 2048, K 8192 on 128 x 128 tiles 86.6 whole, 73.3 in two;
 // 64 x 2048, K 8192 on 64 x 64 tiles 28 whole, 13.2 in eight.
+// fp32 on 64 x 64 and 128 x 128 tiles against 32 x 32: 256 x 256, K 301 8.8, 5.4;
+// 512 x 512, K 512 14.8, 7.6; 1024 x 512, K 1024 22.1, 22.3; 2048 x 2048, K 1024
+// 97, 147.
 struct Cost {
     int tile, most;
     double fixed, unit[4];
 };
+constexpr Cost kNearCost = {32, 4, 3.6, {0.42, 1.1, 1.6, 2.2}};
 constexpr Cost kSmallCost = {64, 2, 2.7, {0.2, 0.38}};
 constexpr Cost kMiddleCost = {128, 2, 5.5, {0.65, 0.93}};
 constexpr Cost kBigCost = {256, 1, 10.0, {1.5}};
@@ -1041,6 +1123,7 @@ double time_of(const Cost& c, const ProductArgs& a, int splits, double slow) {
 // 10.6, 13.3 and 10.3, 18.7, 16.4.
 // Beyond kCopiesMost they would hold more memory than that time is worth.
 constexpr size_t kCopiesMost = size_t(2) << 30;
+constexpr int64_t kNearTiles = 1 << 16;   // none of its wins has more, and a launch takes them
 Plan plan_of(Product kind, const ProductArgs& a) {
     Plan best{FORM_FEW, 1, false, false};
     const Stored sa = stored_a(kind, a), sb = stored_b(kind, a);
@@ -1074,6 +1157,8 @@ Plan plan_of(Product kind, const ProductArgs& a) {
         offer(FORM_ANY, kAnyCost[a.bf16], slow, 0.0, false, false);
         offer(FORM_ANY_64, kAny64Cost[a.bf16], slow, 0.0, false, false);
     }
+    if (!a.bf16 && tiles_of(a.M, a.N, 32, 32) < kNearTiles && time_of(kNearCost, a, 1, 1.0) < least)
+        best = {FORM_NEAR, 1, false, false};
     return best;
 }
 
@@ -1111,6 +1196,12 @@ hipError_t launch_kind(const ProductArgs& a, Form form, hipStream_t s) {
         else if (form == FORM_MIDDLE) e = launch_tiles<MiddleTile>(&product_tiles<KIND, MiddleTile>, a, s);
         else if (form == FORM_SMALL) e = launch_tiles<SmallTile>(&product_tiles<KIND, SmallTile>, a, s);
         else if (form == FORM_FEW) return launch_few(a, s);
+    }
+    if constexpr (std::is_same<T, float>::value) {
+        if (form == FORM_NEAR) {
+            product_near<KIND><<<(unsigned)tiles_of(a.M, a.N, 32, 32), 64 * kNearWaves, 0, s>>>(a);
+            return hipGetLastError();
+        }
     }
     if (form == FORM_ANY) e = launch_any<KIND, T, 128>(a, s);
     else if (form == FORM_ANY_64) e = launch_any<KIND, T, 64>(a, s);
