@@ -1033,15 +1033,23 @@ __global__ __launch_bounds__(64) void product_join(ProductArgs a) {
     f32x16 acc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
-    for (int s = 0; s < a.splits; ++s, p += mb * nb * 1024)
+    constexpr int U = 8;   // parts on their way together (one by one: 0.3 us a part, 6 of 20 where there are 32)
+    for (int s = 0; s < a.splits; s += U) {
+        float4 x[U][4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float4 x = ldg<float4>(p + 256 * q);
-            acc[4 * q] += x.x;
-            acc[4 * q + 1] += x.y;
-            acc[4 * q + 2] += x.z;
-            acc[4 * q + 3] += x.w;
-        }
+        for (int u = 0; u < U; ++u, p += mb * nb * 1024)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[u][q] = s + u < a.splits ? ldg<float4>(p + 256 * q) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                acc[4 * q] += x[u][q].x;
+                acc[4 * q + 1] += x[u][q].y;
+                acc[4 * q + 2] += x[u][q].z;
+                acc[4 * q + 3] += x[u][q].w;
+            }
+    }
     const int64_t m0 = blockIdx.x / nb * 32, n0 = blockIdx.x % nb * 32;
     with_act_of<KIND>(a.act, [&](auto act) {
         each_row_of_8(acc, threadIdx.x, [&](int r, int c, float (&v)[8]) {
@@ -1101,7 +1109,7 @@ struct Cost {
     double fixed, unit[4];
 };
 constexpr Cost kNearCost = {32, 4, 3.6, {0.42, 1.1, 1.6, 2.2}};
-constexpr Cost kSmallCost = {64, 2, 2.7, {0.2, 0.38}};
+constexpr Cost kSmallCost = {64, 2, 2.7, {0.21, 0.38}};
 constexpr Cost kMiddleCost = {128, 2, 5.5, {0.65, 0.93}};
 constexpr Cost kBigCost = {256, 1, 10.0, {1.5}};
 constexpr Cost kAny64Cost[2] = {{64, 4, 2.7, {2.3, 3.2, 4.3, 5.5}}, {64, 4, 2.7, {0.6, 0.9, 1.05, 1.2}}};   // fp32, bf16
@@ -1113,7 +1121,7 @@ double time_of(const Cost& c, const ProductArgs& a, int splits, double slow) {
     const int64_t rounds = tiles / (256 * c.most), left = (tiles % (256 * c.most) + 255) / 256;
     double t = rounds * (c.fixed + units * c.unit[c.most - 1]);
     if (left) t += c.fixed + units * c.unit[left - 1];
-    if (splits > 1) t += 3.0 + (double)splits * a.M * a.N * 8 / 8e6;
+    if (splits > 1) t += 2.5 + 0.1 * splits + (double)splits * a.M * a.N * 8 / 8e6;
     return t;
 }
 
@@ -1149,11 +1157,12 @@ Plan plan_of(Product kind, const ProductArgs& a) {
         offer(FORM_SMALL, kSmallCost, 1.0, more, copy_a, copy_b);
     }
     if (!direct || copy_a || copy_b) {
-        // rows of odd width read across: 1.1 to 2.2 times a unit's time, by 1.4 for
-        // each m/n-contiguous operand
+        // rows of odd width read across: in bf16 1.1 to 2.2 times a unit's time, by
+        // 1.4 for each m/n-contiguous operand; in fp32 up to 1.3
+        const double across = a.bf16 ? 1.4 : 1.15;
         double slow = 1.0;
-        if (a.bf16 && copy_a && kind == PROD_WEIGHT) slow *= 1.4;
-        if (a.bf16 && copy_b && kind != PROD_FORWARD) slow *= 1.4;
+        if (copy_a && kind == PROD_WEIGHT) slow *= across;
+        if (copy_b && kind != PROD_FORWARD) slow *= across;
         offer(FORM_ANY, kAnyCost[a.bf16], slow, 0.0, false, false);
         offer(FORM_ANY_64, kAny64Cost[a.bf16], slow, 0.0, false, false);
     }
