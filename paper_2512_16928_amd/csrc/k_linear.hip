@@ -332,12 +332,14 @@ __global__ __launch_bounds__(kGThreads) void product_any(ProductArgs a) {
 // ones [k][row]; 16-byte chunks are swizzled so that the fragment reads of a
 // sixteenth of a wave (and the transposing reads' 64-byte pieces of four k)
 // fall into distinct LDS banks.
-template <int BM_, int BN_, int BK_, int S_, int WM_, int WN_>
+template <typename T_, int BM_, int BN_, int BK_, int S_, int WM_, int WN_>
 struct Tile {
-    static constexpr int BM = BM_, BN = BN_, BK = BK_, S = S_, WM = WM_, WN = WN_;
+    using T = T_;
+    static constexpr int BM = BM_, BN = BN_, BK = BK_, S = S_, WM = WM_, WN = WN_, E = sizeof(T);
+    static_assert(BK * E == 128, "a slice is 128 bytes of a k-contiguous row");
     static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
-    static constexpr int A_BYTES = BM * BK * 2, STAGE = (BM + BN) * BK * 2;
+    static constexpr int A_BYTES = BM * BK * E, STAGE = (BM + BN) * BK * E;
     static constexpr int LOADS = STAGE / 1024 / WAVES;   // of a wave a slice
     // the epilogue's staging of a wave: 32 rows of its part of the tile, padded
     static constexpr int EPI_ROWS = 32, EPI_LD = TN + 4;
@@ -358,19 +360,20 @@ __device__ __forceinline__ void wait_vmcnt() {
 }
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4)); }
 
-// Rows of an operand: an m/n-contiguous one has them in whole chunks.
-template <bool KMAJOR>
-__device__ __forceinline__ int64_t extent(int64_t rows) { return KMAJOR ? rows : (rows + 7) & ~(int64_t)7; }
+// Rows of an operand: an m/n-contiguous one has them in whole chunks of C.
+template <bool KMAJOR, int C>
+__device__ __forceinline__ int64_t extent(int64_t rows) { return KMAJOR ? rows : (rows + C - 1) & ~(int64_t)(C - 1); }
 
 // One operand of a tile: R rows (m or n), slices of BK. HALF 0, 1: every first,
 // second run of 64 rows of a tile of 2 R (what a wave of a 256-row tile reads
 // in its first, second half); -1: the rows as they are.
-template <int R, int BK, int WAVES, bool KMAJOR, int HALF = -1>
+template <typename T, int R, int BK, int WAVES, bool KMAJOR, int HALF = -1>
 struct Operand {
-    static constexpr int PITCH = KMAJOR ? BK * 2 : R * 2;      // LDS row
+    static constexpr int E = sizeof(T), C = 16 / E;            // bytes an entry, entries a chunk
+    static constexpr int PITCH = KMAJOR ? BK * E : R * E;      // LDS row
     static constexpr int CPR = PITCH / 16;
     static constexpr int RPB = 1024 / PITCH;                   // LDS rows a 1 KB block holds
-    static constexpr int Q = R * BK * 2 / 1024 / WAVES;        // blocks a wave
+    static constexpr int Q = R * BK * E / 1024 / WAVES;        // blocks a wave
     static constexpr uint32_t OUT = 0x80000000u;               // past every descriptor's range
     __amdgpu_buffer_rsrc_t rsrc;
     const unsigned char* base;
@@ -380,24 +383,24 @@ struct Operand {
     int k_left;            // from the slice loaded next on
 
     __device__ __forceinline__ static int swizzle(int row) {
-        return KMAJOR ? (row / (PITCH < 256 ? 256 / PITCH : 1)) % CPR : (row & 3) << (PITCH < 256 ? 1 : 2);
+        return KMAJOR ? (row / (PITCH < 256 ? 256 / PITCH : 1)) % CPR : E == 2 ? (row & 3) << (PITCH < 256 ? 1 : 2) : 0;
     }
     __device__ __forceinline__ static int tile_row(int r) {
         return HALF < 0 ? r : r / 64 * 128 + HALF * 64 + r % 64;
     }
     // p: the operand's first row of the tile and first k; rows: of them that exist
-    __device__ __forceinline__ void init(const uint16_t* p, int64_t ld, int64_t rows, int64_t k, int wave, int lane) {
+    __device__ __forceinline__ void init(const T* p, int64_t ld, int64_t rows, int64_t k, int wave, int lane) {
         const int lr = lane / CPR, slot = lane % CPR;
         const int c = slot ^ swizzle(wave * RPB + lr);   // alike in all of a wave's blocks (an even number of rows apart)
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int r = (wave + q * WAVES) * RPB + lr;
-            const int row = tile_row(KMAJOR ? r : 8 * c);
-            off[q] = row < rows ? (uint32_t)(KMAJOR ? row * ld * 2 + 16 * c : r * ld * 2 + 2 * row) : OUT;
+            const int row = tile_row(KMAJOR ? r : C * c);
+            off[q] = row < rows ? (uint32_t)(KMAJOR ? row * ld * E + 16 * c : r * ld * E + E * row) : OUT;
         }
-        k_lane = KMAJOR ? 8 * c : wave * RPB + lr;
+        k_lane = KMAJOR ? C * c : wave * RPB + lr;
         base = reinterpret_cast<const unsigned char*>(p);
-        step = KMAJOR ? 2 * BK : 2 * BK * ld;
+        step = KMAJOR ? E * BK : E * BK * ld;
         k_left = (int)k;
         rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, (int)0x7ffffff0, 0x00020000);
     }
@@ -541,7 +544,7 @@ struct RowSums {
 };
 
 // The end of a wave's sums: parts as they are, else finished through LDS.
-template <Product KIND, typename T>
+template <Product KIND, typename T, typename E>
 __device__ __forceinline__ void finish_sums(const ProductArgs& a, const f32x16 (&acc)[T::FM][T::FN], unsigned char* lds, int64_t m0,
                                             int64_t n0, bool whole, int wave, int lane) {
     wait_loads<0>();   // none may land in what LDS is used for next
@@ -554,6 +557,18 @@ __device__ __forceinline__ void finish_sums(const ProductArgs& a, const f32x16 (
             for (int j = 0; j < T::FN; ++j) store_part(a, m0 + 32 * i, n0 + 32 * j, acc[i][j], lane);
         return;
     }
+    if constexpr (std::is_same<E, float>::value) {   // 32 bytes a lane as they are
+        with_act_of<KIND>(a.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                for (int j = 0; j < T::FN; ++j)
+                    each_row_of_8(acc[i][j], lane, [&](int r, int c, float (&v)[8]) {
+                        finish8_edge<KIND, decltype(act)::value, false, float>(a, m0 + 32 * i + r, n0 + 32 * j + c, v);
+                    });
+        });
+        return;
+    }
     float* stage = reinterpret_cast<float*>(lds) + wave * T::EPI_ROWS * T::EPI_LD;
     with_act_of<KIND>(a.act, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
@@ -562,19 +577,43 @@ __device__ __forceinline__ void finish_sums(const ProductArgs& a, const f32x16 (
     });
 }
 
+// A lane's 16 bytes of a row of 32, and the MFMAs of two of them: eight
+// consecutive k of bf16 make one; four of fp32 four, lanes 0 .. 31 and 32 .. 63
+// taking k and k + 4 (an order of k that both operands have).
+template <typename T> struct FragmentOf { using Type = bf16x8; };
+template <> struct FragmentOf<float> { using Type = __attribute__((ext_vector_type(4))) float; };
+template <typename T> using Fragment = typename FragmentOf<T>::Type;
+__device__ __forceinline__ void multiply(const Fragment<uint16_t>& b, const Fragment<uint16_t>& a, f32x16& acc) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, acc, 0, 0, 0);
+}
+__device__ __forceinline__ void multiply(const Fragment<float>& b, const Fragment<float>& a, f32x16& acc) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(b[j], a[j], acc, 0, 0, 0);
+}
+
 // The fragments of one or two neighbouring blocks of 32 rows (from `row` on)
-// over a whole slice of 64. The transposing reads are one piece of assembly
+// over a whole slice of 128 bytes. The transposing reads are one piece of assembly
 // that ends with their wait: as the compiler's own loads, each would first wait
 // for every load to LDS still on its way.
-template <typename O, int PITCH, int N>
-__device__ __forceinline__ void read_slice(const unsigned char* lds, int row, int lane, bf16x8 (&f)[4][N], std::true_type) {
+template <typename O, int PITCH, typename F, int N>
+__device__ __forceinline__ void read_slice(const unsigned char* lds, int row, int lane, F (&f)[4][N], std::true_type) {
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int r = row + 32 * i + (lane & 31), c = 2 * kk + (lane >> 5);
-            f[kk][i] = *reinterpret_cast<const bf16x8*>(lds + r * PITCH + 16 * (c ^ O::swizzle(r)));
+            f[kk][i] = *reinterpret_cast<const F*>(lds + r * PITCH + 16 * (c ^ O::swizzle(r)));
         }
+}
+template <typename O, int PITCH, int N>
+__device__ __forceinline__ void read_slice(const unsigned char* lds, int row, int lane, Fragment<float> (&f)[4][N], std::false_type) {
+    const unsigned char* p = lds + 4 * (lane >> 5) * PITCH + 4 * (row + (lane & 31));
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[kk][i][j] = *reinterpret_cast<const float*>(p + (8 * kk + j) * PITCH + 128 * i);
 }
 // A lane of a 16-lane group receives element (i mod 4) of the 8 bytes addressed
 // by source lane 4 e + i / 4, e = 0 .. 3: four consecutive k of its row.
@@ -652,8 +691,9 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t total, uint32_t tm
 template <Product KIND, typename T>
 __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
     constexpr bool AK = KIND != PROD_WEIGHT, BKM = KIND == PROD_FORWARD;
-    using OA = Operand<T::BM, T::BK, T::WAVES, AK>;
-    using OB = Operand<T::BN, T::BK, T::WAVES, BKM>;
+    constexpr bool FINE = T::E == 4;
+    using OA = Operand<typename T::T, T::BM, T::BK, T::WAVES, AK>;
+    using OB = Operand<typename T::T, T::BN, T::BK, T::WAVES, BKM>;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / T::WN * T::TM, wn = wave % T::WN * T::TN;
@@ -667,8 +707,10 @@ __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
     const int64_t k_end = s1 == slices ? a.K : (int64_t)s1 * T::BK;
     OA oa;
     OB ob;
-    oa.init(static_cast<const uint16_t*>(a.A) + (AK ? m0 * a.lda + k0 : k0 * a.lda + m0), a.lda, extent<AK>(a.M) - m0, k_end - k0, wave, lane);
-    ob.init(static_cast<const uint16_t*>(a.B) + (BKM ? n0 * a.ldb + k0 : k0 * a.ldb + n0), a.ldb, extent<BKM>(a.N) - n0, k_end - k0, wave, lane);
+    oa.init(static_cast<const typename T::T*>(a.A) + (AK ? m0 * a.lda + k0 : k0 * a.lda + m0), a.lda, extent<AK, OA::C>(a.M) - m0, k_end - k0,
+            wave, lane);
+    ob.init(static_cast<const typename T::T*>(a.B) + (BKM ? n0 * a.ldb + k0 : k0 * a.ldb + n0), a.ldb, extent<BKM, OB::C>(a.N) - n0, k_end - k0,
+            wave, lane);
     auto request = [&](unsigned char* st) {
 #pragma unroll
         for (int q = 0; q < OA::Q; ++q) oa.load(q, st, wave);
@@ -682,7 +724,7 @@ __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
     f32x16 acc[T::FM][T::FN];
     start_sums<KIND, T>(a, acc, n0 + wn, lane);
     RowSums<T> rows;
-    if constexpr (!AK) rows.init(a, in, tn, wave % T::WN, s0);
+    if constexpr (!AK && !FINE) rows.init(a, in, tn, wave % T::WN, s0);
     const int n = s1 - s0;
 #pragma unroll
     for (int p = 0; p < T::S - 1; ++p) request(lds + p * T::STAGE);
@@ -692,7 +734,7 @@ __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         const unsigned char* st = lds + s % T::S * T::STAGE;
-        bf16x8 fa[4][T::FM], fb[4][T::FN];
+        Fragment<typename T::T> fa[4][T::FM], fb[4][T::FN];
         read_slice<OA, OA::PITCH>(st, wm, lane, fa, std::bool_constant<AK>{});
         read_slice<OB, OB::PITCH>(st + T::A_BYTES, wn, lane, fb, std::bool_constant<BKM>{});
         __builtin_amdgcn_sched_barrier(0);
@@ -703,15 +745,14 @@ __global__ __launch_bounds__(T::THREADS) void product_tiles(ProductArgs a) {
 #pragma unroll
             for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-                for (int j = 0; j < T::FN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[kk][j], fa[kk][i], acc[i][j], 0, 0, 0);
-        if constexpr (!AK) {
+                for (int j = 0; j < T::FN; ++j) multiply(fb[kk][j], fa[kk][i], acc[i][j]);
+        if constexpr (!AK && !FINE) {
             if (rows.mine()) rows.add(fa, 0);
             rows.next();
         }
     }
-    if constexpr (!AK) rows.store(a, in, tn, wave % T::WN, m0 + wm, lane);
-    finish_sums<KIND, T>(a, acc, lds, m0 + wm, n0 + wn, m0 + T::BM <= a.M && n0 + T::BN <= a.N, wave, lane);
+    if constexpr (!AK && !FINE) rows.store(a, in, tn, wave % T::WN, m0 + wm, lane);
+    finish_sums<KIND, T, typename T::T>(a, acc, lds, m0 + wm, n0 + wn, m0 + T::BM <= a.M && n0 + T::BN <= a.N, wave, lane);
 }
 
 // 256 x 256 tiles, eight waves in two groups of four, one of each group on
@@ -746,9 +787,9 @@ template <Product KIND>
 __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a) {
     using T = PairTile;
     constexpr bool AK = KIND != PROD_WEIGHT, BKM = KIND == PROD_FORWARD;
-    using O0 = Operand<T::BM / 2, T::BK, T::WAVES, AK, 0>;
-    using O1 = Operand<T::BM / 2, T::BK, T::WAVES, AK, 1>;
-    using OB = Operand<T::BN, T::BK, T::WAVES, BKM>;
+    using O0 = Operand<uint16_t, T::BM / 2, T::BK, T::WAVES, AK, 0>;
+    using O1 = Operand<uint16_t, T::BM / 2, T::BK, T::WAVES, AK, 1>;
+    using OB = Operand<uint16_t, T::BN, T::BK, T::WAVES, BKM>;
     static_assert(O0::Q == 2 && O1::Q == 2 && OB::Q == 4, "loads of a wave a slice: 6 and 2");
     extern __shared__ __align__(1024) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -767,9 +808,9 @@ __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a
     O0 o0;
     O1 o1;
     OB ob;
-    o0.init(A, a.lda, extent<AK>(a.M) - m0, k, wave, lane);
-    o1.init(A, a.lda, extent<AK>(a.M) - m0, k, wave, lane);
-    ob.init(B, a.ldb, extent<BKM>(a.N) - n0, k, wave, lane);
+    o0.init(A, a.lda, extent<AK, 8>(a.M) - m0, k, wave, lane);
+    o1.init(A, a.lda, extent<AK, 8>(a.M) - m0, k, wave, lane);
+    ob.init(B, a.ldb, extent<BKM, 8>(a.N) - n0, k, wave, lane);
     // a stage: A's first half, its second, B
     auto request_first = [&](unsigned char* st) {
 #pragma unroll
@@ -855,7 +896,7 @@ __global__ __launch_bounds__(PairTile::THREADS) void product_pairs(ProductArgs a
     }
     if (!second) swap();
     if constexpr (!AK) rows.store(a, in, tn, wn, m0 + wm * T::TM, lane);
-    finish_sums<KIND, T>(a, acc, lds, m0 + wm * T::TM, n0 + wn * T::TN, m0 + T::BM <= a.M && n0 + T::BN <= a.N, wave, lane);
+    finish_sums<KIND, T, uint16_t>(a, acc, lds, m0 + wm * T::TM, n0 + wn * T::TN, m0 + T::BM <= a.M && n0 + T::BN <= a.N, wave, lane);
 }
 
 // ----------------------------------------------------------- few tokens
@@ -1008,7 +1049,7 @@ __global__ __launch_bounds__(64 * kNearWaves) void product_near(ProductArgs a) {
 }
 
 // Copies of operands in whole chunks of 16 bytes, zeros behind each row: a chunk
-// a thread; blockIdx.y is the operand.
+// a thread; blockIdx.y is the operand. ld and width count two bytes.
 struct CopyArgs {
     const uint16_t* from[2];
     uint16_t* to[2];
@@ -1058,8 +1099,8 @@ __global__ __launch_bounds__(64) void product_join(ProductArgs a) {
     });
 }
 
-typedef Tile<128, 128, 64, 2, 2, 2> MiddleTile;
-typedef Tile<64, 64, 64, 4, 2, 2> SmallTile;
+template <typename T> using MiddleTile = Tile<T, 128, 128, 128 / sizeof(T), 2, 2, 2>;
+template <typename T> using SmallTile = Tile<T, 64, 64, 128 / sizeof(T), 4, 2, 2>;
 
 enum Form { FORM_ANY, FORM_ANY_64, FORM_NEAR, FORM_FEW, FORM_SMALL, FORM_MIDDLE, FORM_BIG };
 struct Plan {
@@ -1072,20 +1113,22 @@ struct Plan {
 struct Stored {
     const void* p;
     int64_t ld, outer, inner;
+    int e;   // bytes an entry
     // Rows are whole chunks of 16 bytes from one 16-byte boundary to the next.
     // Sizes and pitches alone say whether a copy is needed, so that the
     // workspace can be told in advance; of the others the pointer must be aligned.
-    bool whole() const { return ld % 8 == 0 && inner % 8 == 0 && ld < (int64_t(1) << 21); }
+    bool whole() const { return ld * e % 16 == 0 && inner * e % 16 == 0 && ld < (int64_t(1) << 21); }
     bool aligned() const { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-    size_t copy_bytes() const { return ((size_t)outer * ((inner + 7) / 8 * 16) + 255) & ~size_t(255); }
+    int64_t chunks() const { return (inner * e + 15) / 16; }   // a row
+    size_t copy_bytes() const { return ((size_t)outer * chunks() * 16 + 255) & ~size_t(255); }
 };
 Stored stored_a(Product kind, const ProductArgs& a) {
-    if (kind == PROD_WEIGHT) return {a.A, a.lda, a.K, a.M};
-    return {a.A, a.lda, a.M, a.K};
+    if (kind == PROD_WEIGHT) return {a.A, a.lda, a.K, a.M, a.bf16 ? 2 : 4};
+    return {a.A, a.lda, a.M, a.K, a.bf16 ? 2 : 4};
 }
 Stored stored_b(Product kind, const ProductArgs& a) {
-    if (kind == PROD_FORWARD) return {a.B, a.ldb, a.N, a.K};
-    return {a.B, a.ldb, a.K, a.N};
+    if (kind == PROD_FORWARD) return {a.B, a.ldb, a.N, a.K, a.bf16 ? 2 : 4};
+    return {a.B, a.ldb, a.K, a.N, a.bf16 ? 2 : 4};
 }
 
 int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
@@ -1109,10 +1152,10 @@ struct Cost {
     double fixed, unit[4];
 };
 constexpr Cost kNearCost = {32, 4, 3.6, {0.42, 1.1, 1.6, 2.2}};
-constexpr Cost kSmallCost = {64, 2, 2.7, {0.21, 0.38}};
-constexpr Cost kMiddleCost = {128, 2, 5.5, {0.65, 0.93}};
+constexpr Cost kSmallCost[2] = {{64, 2, 2.7, {1.0, 2.0}}, {64, 2, 2.7, {0.21, 0.38}}};   // fp32, bf16
+constexpr Cost kMiddleCost[2] = {{128, 2, 4.0, {4.0, 7.5}}, {128, 2, 5.5, {0.65, 0.93}}};
 constexpr Cost kBigCost = {256, 1, 10.0, {1.5}};
-constexpr Cost kAny64Cost[2] = {{64, 4, 2.7, {2.3, 3.2, 4.3, 5.5}}, {64, 4, 2.7, {0.6, 0.9, 1.05, 1.2}}};   // fp32, bf16
+constexpr Cost kAny64Cost[2] = {{64, 4, 2.7, {2.3, 3.2, 4.3, 5.5}}, {64, 4, 2.7, {0.6, 0.9, 1.05, 1.2}}};
 constexpr Cost kAnyCost[2] = {{128, 2, 4.0, {6.1, 10.4}}, {128, 2, 4.0, {1.5, 2.0}}};
 
 double time_of(const Cost& c, const ProductArgs& a, int splits, double slow) {
@@ -1137,7 +1180,7 @@ Plan plan_of(Product kind, const ProductArgs& a) {
     const Stored sa = stored_a(kind, a), sb = stored_b(kind, a);
     const bool copy_a = !sa.whole(), copy_b = !sb.whole();
     const size_t copied = (copy_a ? sa.copy_bytes() : 0) + (copy_b ? sb.copy_bytes() : 0);
-    const bool direct = a.bf16 && (copy_a || sa.aligned()) && (copy_b || sb.aligned()) && copied <= kCopiesMost;
+    const bool direct = (copy_a || sa.aligned()) && (copy_b || sb.aligned()) && copied <= kCopiesMost;
     if (a.bf16 && kind == PROD_FORWARD && a.M <= 32) return best;
     double least = 0.0;
     // slow: of the units; more: us once
@@ -1152,9 +1195,9 @@ Plan plan_of(Product kind, const ProductArgs& a) {
     };
     if (direct) {
         const double more = copy_a || copy_b ? 5.0 + 2.0 * copied / 4e6 : 0.0;
-        offer(FORM_BIG, kBigCost, 1.0, more, copy_a, copy_b);
-        offer(FORM_MIDDLE, kMiddleCost, 1.0, more, copy_a, copy_b);
-        offer(FORM_SMALL, kSmallCost, 1.0, more, copy_a, copy_b);
+        if (a.bf16) offer(FORM_BIG, kBigCost, 1.0, more, copy_a, copy_b);
+        offer(FORM_MIDDLE, kMiddleCost[a.bf16], 1.0, more, copy_a, copy_b);
+        offer(FORM_SMALL, kSmallCost[a.bf16], 1.0, more, copy_a, copy_b);
     }
     if (!direct || copy_a || copy_b) {
         // rows of odd width read across: in bf16 1.1 to 2.2 times a unit's time, by
@@ -1202,8 +1245,6 @@ hipError_t launch_kind(const ProductArgs& a, Form form, hipStream_t s) {
     hipError_t e = hipSuccess;
     if constexpr (std::is_same<T, uint16_t>::value) {
         if (form == FORM_BIG) e = launch_tiles<PairTile>(&product_pairs<KIND>, a, s);
-        else if (form == FORM_MIDDLE) e = launch_tiles<MiddleTile>(&product_tiles<KIND, MiddleTile>, a, s);
-        else if (form == FORM_SMALL) e = launch_tiles<SmallTile>(&product_tiles<KIND, SmallTile>, a, s);
         else if (form == FORM_FEW) return launch_few(a, s);
     }
     if constexpr (std::is_same<T, float>::value) {
@@ -1212,7 +1253,9 @@ hipError_t launch_kind(const ProductArgs& a, Form form, hipStream_t s) {
             return hipGetLastError();
         }
     }
-    if (form == FORM_ANY) e = launch_any<KIND, T, 128>(a, s);
+    if (form == FORM_MIDDLE) e = launch_tiles<MiddleTile<T>>(&product_tiles<KIND, MiddleTile<T>>, a, s);
+    else if (form == FORM_SMALL) e = launch_tiles<SmallTile<T>>(&product_tiles<KIND, SmallTile<T>>, a, s);
+    else if (form == FORM_ANY) e = launch_any<KIND, T, 128>(a, s);
     else if (form == FORM_ANY_64) e = launch_any<KIND, T, 64>(a, s);
     if (e != hipSuccess || a.splits == 1) return e;
     product_join<KIND, T><<<(unsigned)tiles_of(a.M, a.N, 32, 32), 64, 0, s>>>(a);
@@ -1238,10 +1281,10 @@ hipError_t make_copies(Product kind, ProductArgs& a, const Plan& p, hipStream_t 
     auto add = [&](const Stored& o, const void** pointer, int64_t* ld) {
         c.from[n] = static_cast<const uint16_t*>(o.p);
         c.to[n] = reinterpret_cast<uint16_t*>(to);
-        c.ld[n] = o.ld; c.rows[n] = o.outer; c.width[n] = o.inner;
-        chunks = std::max(chunks, o.outer * ((o.inner + 7) / 8));
+        c.ld[n] = o.ld * o.e / 2; c.rows[n] = o.outer; c.width[n] = o.inner * o.e / 2;
+        chunks = std::max(chunks, o.outer * o.chunks());
         *pointer = to;
-        *ld = (o.inner + 7) / 8 * 8;
+        *ld = o.chunks() * 16 / o.e;
         to += o.copy_bytes();
         ++n;
     };
@@ -1264,7 +1307,7 @@ size_t product_workspace(Product kind, const ProductArgs& a) { return plan_bytes
 
 int64_t product_row_sums(const ProductArgs& a) {
     const Plan p = plan_of(PROD_WEIGHT, a);
-    const int tile = p.form == FORM_BIG ? 256 : p.form == FORM_MIDDLE ? 128 : p.form == FORM_SMALL ? 64 : 0;
+    const int tile = !a.bf16 ? 0 : p.form == FORM_BIG ? 256 : p.form == FORM_MIDDLE ? 128 : p.form == FORM_SMALL ? 64 : 0;
     const int waves = p.form == FORM_BIG ? PairTile::WN : 2;
     return tile ? (int64_t)p.splits * waves * ((a.N + tile - 1) / tile) : 0;
 }
