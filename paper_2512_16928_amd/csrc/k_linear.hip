@@ -321,17 +321,17 @@ __global__ __launch_bounds__(kGThreads) void product_any(ProductArgs a) {
     });
 }
 
-// -------------------------------------------------- bf16 tiles, LDS fed directly
+// ------------------------------------------------------- tiles, LDS fed directly
 // For operands whose rows start on 16-byte boundaries and are whole chunks of 16
 // bytes long (others are copied so first, with zeros behind). K-slices go from
 // global memory straight into LDS (16 bytes a lane, a wave's 1 KB a time), S
 // slices in flight, through buffer descriptors: a lane whose chunk lies past
 // an edge asks for an offset past the descriptor's range and gets zeros.
 //
-// k-contiguous tiles are kept [row][k] in rows of 2 BK bytes, m/n-contiguous
+// k-contiguous tiles are kept [row][k] in rows of 128 bytes, m/n-contiguous
 // ones [k][row]; 16-byte chunks are swizzled so that the fragment reads of a
 // sixteenth of a wave (and the transposing reads' 64-byte pieces of four k)
-// fall into distinct LDS banks.
+// fall into distinct LDS banks. fp32's [k][row] is read an entry a lane.
 template <typename T_, int BM_, int BN_, int BK_, int S_, int WM_, int WN_>
 struct Tile {
     using T = T_;
@@ -1144,9 +1144,9 @@ int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return ((M + bm - 1) / 
 // A product cut into parts adds their round trip through the caches at 8 TB/s
 // and a launch: 2048 x 2048, K 8192 on 128 x 128 tiles 86.6 whole, 73.3 in two;
 // 64 x 2048, K 8192 on 64 x 64 tiles 28 whole, 13.2 in eight.
-// fp32 on 64 x 64 and 128 x 128 tiles against 32 x 32: 256 x 256, K 301 8.8, 5.4;
-// 512 x 512, K 512 14.8, 7.6; 1024 x 512, K 1024 22.1, 22.3; 2048 x 2048, K 1024
-// 97, 147.
+// fp32 on tiles of 32, 64, 128 and, through registers, 64 and 128: 301 x 256, K 256
+// 5.7, 7.9, -, 8.9, -; 512 x 512, K 512 7.8, 10.7, -, 12.7, -; 2048 x 512, K 512 22.6,
+// 13.3, -, 22.2, -; 2048 x 2048, K 2048 -, 143, 137, -, 177.
 struct Cost {
     int tile, most;
     double fixed, unit[4];
@@ -1171,7 +1171,7 @@ double time_of(const Cost& c, const ProductArgs& a, int splits, double slow) {
 // Copies cost a launch and their bytes at 4 TB/s. Forward, input and weight
 // gradient of 8191 tokens through 2047 x 2041: 78, 75 and 103 us with copies, on
 // tiles of any alignment 144, 202 and 284; 1531 tokens through 1000 x 517: 12.5,
-// 10.6, 13.3 and 10.3, 18.7, 16.4.
+// 10.6, 13.3 and 10.3, 18.7, 16.4, in fp32 30, 28, 36 and 32, 35, 39.
 // Beyond kCopiesMost they would hold more memory than that time is worth.
 constexpr size_t kCopiesMost = size_t(2) << 30;
 constexpr int64_t kNearTiles = 1 << 16;   // none of its wins has more, and a launch takes them
