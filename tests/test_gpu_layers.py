@@ -621,6 +621,27 @@ def test_odd_widths_with_the_callers_workspace(hip_device, t, r, c):
     assert bool((ws[need:] == 0xFF).all())
 
 
+@pytest.mark.parametrize("t,r,c", [(300, 131, 517), (2500, 2051, 77), (3000, 131, 2055), (130, 1027, 1029), (1500, 1001, 1003)])
+def test_odd_fp32_widths_with_the_callers_workspace(hip_device, t, r, c):
+    """The same in fp32, where whole rows are multiples of four, against 64 bits; the workspace ends where it is said to."""
+    g = gen_of("oddf", t, r, c)
+    X, dY = Framed(t, c, F32, 4, 2, rnd((t, c), F32, g)).view, Framed(t, r, F32, 1, 1, rnd((t, r), F32, g, 1e-2)).view
+    W, Y, dX = rnd((r, c), F32, g, 0.1), Framed(t, r, F32, 4, 3), Framed(t, c, F32, 2, 1)
+    G, db = torch.empty((r, c), device="cuda"), torch.empty(r, device="cuda")
+    need = binding.dion2_linear_workspace_size(t, r, c, F32, ld_x=c + 2, ld_dy=r + 1)
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda")      # NaN wherever it is read unwritten
+    for _ in range(2):
+        binding.dion2_linear_forward(Y.view, X, W, workspace=ws[:need])
+        near(Y.view, *product64(X, W), F32, "Y")
+        binding.dion2_linear_backward_input(dX.view, dY, W, workspace=ws[:need])
+        near(dX.view, *product64(dY, W.t()), F32, "dX")
+        binding.dion2_linear_backward_weight(G, dY, X, dbias=db, workspace=ws[:need])
+        near(G, *product64(dY.t(), X.t()), F32, "G")
+        near(db, dY.double().sum(0), (t + 16) * 2.0 ** -23 * dY.double().abs().sum(0), F32, "dbias")
+        ws[:need] = 0xFF
+    assert Y.intact() and dX.intact() and bool((ws[need:] == 0xFF).all())
+
+
 @pytest.mark.parametrize("cols", [5, 264, 2041, 5123])
 @pytest.mark.parametrize("t", [1, 7, 16, 17, 32])
 def test_few_tokens_of_any_width(hip_device, t, cols):
