@@ -344,6 +344,25 @@ def test_layernorm_backward(hip_device, i, dtype):
     assert torch.equal(dY, dX.view)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("r,c", [(72, 40), (131, 77), (1032, 1040), (2056, 2056)])
+def test_linear_calls_without_tokens(hip_device, r, c, dtype):
+    """Gradients are sums of nothing, on every form of tile; the other calls write nothing."""
+    X, dY = torch.empty((0, c), dtype=dtype, device="cuda"), torch.empty((0, r), dtype=dtype, device="cuda")
+    W, Y, dX = torch.ones((r, c), dtype=dtype, device="cuda"), torch.empty_like(dY), torch.empty_like(X)
+    binding.dion2_linear_forward(Y, X, W)
+    binding.dion2_linear_backward_input(dX, dY, W)
+    for g_dtype in (BF, F32):
+        G, db = torch.full((r, c), 2.0, dtype=g_dtype, device="cuda"), torch.full((r,), 2.0, dtype=g_dtype, device="cuda")
+        binding.dion2_linear_backward_weight(G, dY, X, dbias=db, accumulate=True)
+        assert bool((G == 2).all()) and bool((db == 2).all())
+        binding.dion2_linear_backward_weight(G, dY, X, dbias=db)
+        assert bool((G == 0).all()) and bool((db == 0).all())
+        db.fill_(2.0)
+        binding.dion2_linear_backward_weight(None, dY, None, dbias=db)
+        assert bool((db == 0).all())
+
+
 def test_layernorm_backward_without_tokens(hip_device):
     z = torch.zeros((0, 40), device="cuda")
     s = torch.zeros(0, device="cuda")
