@@ -519,9 +519,10 @@ int dion2_layernorm_backward(void* dX, void* dgamma, void* dbeta, const void* dY
 /* Bytes of workspace that suffice for every linear call (every norm call) of
    these sizes with opt's dtype and, for the linear calls, its ld_x and ld_dy; 0
    where none is needed or the sizes or types are invalid. Linear calls use it
-   for parts of a sum over few output tiles, and for copies of operands whose
-   width or pitch is no multiple of 16 bytes (which then run at the speed of
-   those whose is), 2 GiB of copies at most. */
+   for parts of a sum over few output tiles (512 MiB at most), for copies of
+   operands whose width or pitch is no multiple of 16 bytes (which then run at
+   the speed of those whose is; 2 GiB at most), and for the bias gradient's
+   partial sums. */
 size_t dion2_linear_workspace_size(int64_t tokens, int64_t rows, int64_t cols,
                                    const dion2_layer_options* opt);
 size_t dion2_layernorm_workspace_size(int64_t tokens, int64_t cols,

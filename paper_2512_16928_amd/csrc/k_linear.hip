@@ -1136,6 +1136,8 @@ Stored stored_b(Product kind, const ProductArgs& a) {
 
 int64_t tiles_of(int64_t M, int64_t N, int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); }
 
+size_t part_bytes(const ProductArgs& a, int splits) { return splits > 1 ? (size_t)splits * tiles_of(a.M, a.N, 32, 32) * 4096 : 0; }
+
 // A launch's time by its tiles: 256 CUs take up to `most` tiles each at a time,
 // and such a round lasts `fixed` us (the start and the epilogue) plus, for every
 // 64 of K, unit[n - 1] us where a CU holds n tiles. Measured in graphs of 30
@@ -1177,6 +1179,12 @@ double time_of(const Cost& c, const ProductArgs& a, int splits, double slow) {
 // 10.6, 13.3 and 10.3, 18.7, 16.4, in fp32 30, 28, 36 and 32, 35, 39.
 // Beyond kCopiesMost they would hold more memory than that time is worth.
 constexpr size_t kCopiesMost = size_t(2) << 30;
+// Parts are for few output tiles: on 512 of 256 x 256 (two rounds) four of them
+// are 512 MiB. More is refused, and so is a cut that by the model gains less than a
+// twentieth over the same tiles' whole sums, well inside what it is off by: 262144 tokens through 32000 x 8192 would
+// take 4 GB of parts for 0.02% of their 98 ms.
+constexpr size_t kPartsMost = size_t(512) << 20;
+constexpr double kPartsWorth = 1.05;
 constexpr int64_t kNearTiles = 1 << 16;   // none of its wins has more, and a launch takes them
 Plan plan_of(Product kind, const ProductArgs& a) {
     Plan best{FORM_FEW, 1, false, false};
@@ -1188,8 +1196,11 @@ Plan plan_of(Product kind, const ProductArgs& a) {
     double least = 0.0;
     // slow: of the units; more: us once
     auto offer = [&](Form form, const Cost& c, double slow, double more, bool ca, bool cb) {
+        const double whole = time_of(c, a, 1, slow) + more;
         for (int splits = 1; splits <= 32 && (splits == 1 || (a.K + 63) / 64 >= splits); splits *= 2) {
-            const double t = time_of(c, a, splits, slow) + more;
+            if (part_bytes(a, splits) > kPartsMost) break;
+            const double t = splits == 1 ? whole : time_of(c, a, splits, slow) + more;
+            if (splits > 1 && t * kPartsWorth > whole) continue;
             if (best.form == FORM_FEW || t < least) {
                 best = {form, splits, ca, cb};
                 least = t;
@@ -1300,8 +1311,7 @@ hipError_t make_copies(Product kind, ProductArgs& a, const Plan& p, hipStream_t 
 }
 
 size_t plan_bytes(Product kind, const ProductArgs& a, const Plan& p) {
-    const size_t parts = p.splits > 1 ? (size_t)p.splits * tiles_of(a.M, a.N, 32, 32) * 4096 : 0;
-    return copy_bytes(kind, a, p) + parts;
+    return copy_bytes(kind, a, p) + part_bytes(a, p.splits);
 }
 
 }  // namespace
