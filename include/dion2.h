@@ -418,10 +418,11 @@ int dion2_plan_form(int batch, int64_t rows, int64_t cols, float alpha,
  *     run on bf16 MFMA (exact products), those of fp32 operands on fp32 MFMA.
  *   - Sums are taken in an order fixed by the sizes, the type and whether
  *     pointers and pitches allow 16-byte loads: runs repeat bitwise. No atomics.
- *   - Activations are evaluated in fp32, Phi within 1e-6 relative for |z| <= 4
- *     (4e-6 for |z| <= 9) in fp32 calls and 1e-5 in bf16 ones, from Z's sums
- *     before rounding in dion2_linear_forward and from the stored Z in the
- *     gradients. An infinite z gives what the formula gives (gelu(+inf) = inf,
+ *   - Activations are evaluated in fp32, GELU's Phi(-|z|) within 1.5e-6 relative
+ *     for |z| <= 4, 5e-6 for |z| <= 9 and 1e-5 for |z| <= 12 (beyond, it is
+ *     below 2e-33 and so is what it is off by), from Z's sums before rounding
+ *     in dion2_linear_forward and from the stored Z in the gradients. An
+ *     infinite z gives what the formula gives (gelu(+inf) = inf,
  *     gelu(-inf) = NaN). A NaN or infinity reaches the outputs whose sums it
  *     is part of and no others.
  *

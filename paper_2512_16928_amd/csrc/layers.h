@@ -13,42 +13,31 @@ namespace dion2 {
 enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SILU = 4 };
 
 // -------------------------------------------------------------- activations
-// Phi(x) = erfc(-x / sqrt 2) / 2 from erfc(u) = t e^{-u^2} P(t), t = 1 / (1 + p u),
-// u >= 0, so neither tail cancels. P is a polynomial fitted here by weighted
-// least squares (Lawson's iteration) to erfc(u) e^{u^2} / t for the smallest
-// largest relative error on u <= 10: with bf16 activations of degree 5, 8.4e-6
-// (bf16's half step is 2^-8 = 3.9e-3), with fp32 ones of degree 8, 2e-8.
-// Evaluated in fp32 the result is within 1e-6 relative for |x| <= 4 and 4e-6
-// for |x| <= 9 (degree 8; the rounding of x^2 grows through the exponential),
-// 1e-5 (degree 5). The value is for -|x|, and with SLOPE that of
-// Phi(x) + x phi(x) for it, which takes no second exponential: either is for
-// x > 0 one less what it is there.
+// Phi(x) = erfc(-x / sqrt 2) / 2 from erfc(u) = t e^{-u^2} P(t), t = 1 / (1 + 0.3 u),
+// u >= 0, so neither tail cancels. P is a polynomial of degree 8 fitted here by
+// weighted least squares (Lawson's iteration) to erfc(u) e^{u^2} / t for the
+// smallest largest relative error on u <= 10, 2e-8. Evaluated in fp32 the result
+// is within 1.5e-6 relative for |x| <= 4, 5e-6 for |x| <= 9 and 1e-5 for |x| <= 12
+// (the rounding of x^2 grows through the exponential; beyond it is below 2e-33).
+// The value is for -|x|, and with SLOPE that of Phi(x) + x phi(x) for it,
+// which takes no second exponential: either is for x > 0 one less what it is there.
+// FINE (fp32 calls), here and in logistic(): a division, where the reciprocal
+// instruction is off by up to a unit of fp32's last place.
 template <bool FINE, bool SLOPE>
 __device__ __forceinline__ float normal_cdf(float x) {
     const float u = __builtin_fabsf(x);
     const float e = __builtin_amdgcn_exp2f(-0.72134752f * x * x);
-    float p;
-    float t;
-    if constexpr (FINE) {
-        t = 1.0f / __builtin_fmaf(0.21213203f, u, 1.0f);   // 0.3 / sqrt 2
-        p = -0.0647770372f;             // P's coefficients, halved
-        p = __builtin_fmaf(p, t, 0.2428634512f);
-        p = __builtin_fmaf(p, t, -0.2563233373f);
-        p = __builtin_fmaf(p, t, 0.2740919430f);
-        p = __builtin_fmaf(p, t, -0.0475035953f);
-        p = __builtin_fmaf(p, t, 0.1075485246f);
-        p = __builtin_fmaf(p, t, 0.0741446257f);
-        p = __builtin_fmaf(p, t, 0.0853616619f);
-        p = __builtin_fmaf(p, t, 0.0845937237f);
-    } else {
-        t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.45961941f, u, 1.0f));   // 0.65 / sqrt 2
-        p = 0.0721254741f;
-        p = __builtin_fmaf(p, t, -0.2366525800f);
-        p = __builtin_fmaf(p, t, 0.1786361119f);
-        p = __builtin_fmaf(p, t, 0.1157274012f);
-        p = __builtin_fmaf(p, t, 0.1869775786f);
-        p = __builtin_fmaf(p, t, 0.1831902260f);
-    }
+    const float d = __builtin_fmaf(0.21213203f, u, 1.0f);   // 0.3 / sqrt 2
+    const float t = FINE ? 1.0f / d : __builtin_amdgcn_rcpf(d);
+    float p = -0.0647770372f;             // P's coefficients, halved
+    p = __builtin_fmaf(p, t, 0.2428634512f);
+    p = __builtin_fmaf(p, t, -0.2563233373f);
+    p = __builtin_fmaf(p, t, 0.2740919430f);
+    p = __builtin_fmaf(p, t, -0.0475035953f);
+    p = __builtin_fmaf(p, t, 0.1075485246f);
+    p = __builtin_fmaf(p, t, 0.0741446257f);
+    p = __builtin_fmaf(p, t, 0.0853616619f);
+    p = __builtin_fmaf(p, t, 0.0845937237f);
     const float h = (SLOPE ? __builtin_fmaf(p, t, -0.39894228f * u) : p * t) * e;
     return x > 0.0f ? 1.0f - h : h;
 }
