@@ -77,10 +77,14 @@
  *     any error nothing is modified and a negative dion2_status is returned.
  *     dion2_last_error() gives a message for the calling thread.
  *   - Without a caller workspace the library keeps one internal workspace
- *     per (device, stream) and grows it with hipMalloc when needed (the
- *     growth synchronises the device). Concurrent calls on different
- *     streams use different workspaces; concurrent calls on one stream
- *     from several host threads are serialised by a lock.
+ *     per (device, stream) for steps and one for layer calls, and grows them
+ *     with hipMalloc when needed (the growth synchronises the device).
+ *     Concurrent calls on different streams use different workspaces;
+ *     concurrent calls on one stream from several host threads are
+ *     serialised by a lock. A HIP graph that holds a step captured with the
+ *     library's workspace may be replayed until a later step on that stream
+ *     needs a larger one or dion2_release_workspaces is called; layer calls
+ *     do not touch it.
  *   - Limits: 1 <= rows, cols; rows * cols < 2^31; 1 <= batch <= 65535;
  *     0 < alpha <= 1; 0 <= ns_steps <= DION2_MAX_NS_STEPS; mu, lr finite.
  */

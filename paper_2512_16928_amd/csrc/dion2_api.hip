@@ -18,6 +18,7 @@
 #include <map>
 #include <mutex>
 #include <string>
+#include <tuple>
 #include <utility>
 #include <vector>
 
@@ -238,12 +239,16 @@ int ensure_aux(Workspace* w, int n, int m) {
     return DION2_OK;
 }
 
+// The steps of a stream share one, its layer calls another: a captured step
+// replays on the addresses it was captured with, and no layer call between two
+// replays may take these away by growing the block, or write there out of turn.
+enum class Calls { STEPS, LAYERS };
 std::mutex g_ws_mutex;
-std::map<std::pair<int, hipStream_t>, Workspace*> g_ws;
+std::map<std::tuple<int, hipStream_t, Calls>, Workspace*> g_ws;
 
-Workspace* workspace_for(int dev, hipStream_t s) {
+Workspace* workspace_for(int dev, hipStream_t s, Calls calls) {
     std::lock_guard<std::mutex> lk(g_ws_mutex);
-    auto& w = g_ws[{dev, s}];
+    auto& w = g_ws[{dev, s, calls}];
     if (!w) w = new Workspace();
     return w;
 }
@@ -272,11 +277,11 @@ int ensure_device(Workspace* w, size_t bytes) {
 
 namespace dion2 {
 
-int lease_workspace(hipStream_t s, size_t bytes, WorkspaceLease* out) {
+int lease_layer_workspace(hipStream_t s, size_t bytes, WorkspaceLease* out) {
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
-    Workspace* w = workspace_for(dev, s);
+    Workspace* w = workspace_for(dev, s, Calls::LAYERS);
     out->lock = std::unique_lock<std::mutex>(w->use);
     int st = ensure_device(w, bytes);
     if (st == DION2_OK) out->dev = static_cast<char*>(w->dev);
@@ -1148,7 +1153,7 @@ int run_step(const Plan& P, void* W, float* M, const void* G, const Tables* tabs
     if (opt.workspace) {
         ws = static_cast<char*>(opt.workspace);
     } else {
-        w = workspace_for(dev, stream);
+        w = workspace_for(dev, stream, Calls::STEPS);
         use_lock = std::unique_lock<std::mutex>(w->use);
         int st = ensure_device(w, P.total);
         if (st != DION2_OK) return st;
@@ -1477,7 +1482,7 @@ int groups_impl(const dion2_group* groups, int ngroups, float alpha, float mu, f
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
-    Workspace* w = workspace_for(dev, stream);
+    Workspace* w = workspace_for(dev, stream, Calls::STEPS);
     std::unique_lock<std::mutex> use_lock(w->use);
     st = ensure_device(w, total);
     if (st != DION2_OK) return st;
@@ -1778,7 +1783,7 @@ void dion2_release_workspaces(void) {
         Workspace* w = kv.second;
         std::lock_guard<std::mutex> use(w->use);
         // best effort: a failure here leaves memory to the process's end
-        if (hipSetDevice(kv.first.first) == hipSuccess) (void)hipDeviceSynchronize();
+        if (hipSetDevice(std::get<0>(kv.first)) == hipSuccess) (void)hipDeviceSynchronize();
         if (w->dev) (void)hipFree(w->dev);
         for (TableSlot& c : w->slots) {
             if (c.host) (void)hipHostFree(c.host);

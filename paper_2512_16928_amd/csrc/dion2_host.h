@@ -16,12 +16,13 @@ constexpr int64_t kMaxDim = int64_t(1) << 20;   // longest side of a weight matr
 int fail(int status, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 int hip_fail(hipError_t e, const char* what);
 
-// A call's hold on the library workspace of (current device, stream): at
-// least the bytes asked for, kept from other host threads while it lives.
+// A layer call's hold on the library workspace that (current device, stream)
+// has for these calls, apart from the steps': at least the bytes asked for, kept
+// from other host threads while it lives.
 struct WorkspaceLease {
     std::unique_lock<std::mutex> lock;
     char* dev = nullptr;
 };
-int lease_workspace(hipStream_t s, size_t bytes, WorkspaceLease* out);
+int lease_layer_workspace(hipStream_t s, size_t bytes, WorkspaceLease* out);
 
 }  // namespace dion2

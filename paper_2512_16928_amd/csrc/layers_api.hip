@@ -153,7 +153,7 @@ int take_scratch(const dion2_layer_options& o, size_t bytes, hipStream_t s, Scra
     if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
     if (cap != hipStreamCaptureStatusNone)
         return fail(DION2_ERR_WORKSPACE, "a captured call needs the caller's workspace (%zu bytes)", bytes);
-    int st = lease_workspace(s, bytes, &out->lease);
+    int st = lease_layer_workspace(s, bytes, &out->lease);
     out->p = out->lease.dev;
     return st;
 }
