@@ -1,6 +1,8 @@
 """What the linear calls ask for in workspace: host arithmetic, no GPU needed."""
+import ctypes
 import os
 import random
+import re
 
 import pytest
 import torch
@@ -46,3 +48,44 @@ def test_few_tiles_keep_their_parts():
     for t, r, c in ((72, 520, 8200), (2048, 2048, 8192), (64, 2048, 8192)):
         assert binding.dion2_linear_workspace_size(t, r, c, BF) >= 2 * t * r * 4
     assert binding.dion2_linear_workspace_size(1 << 18, 128, 128, F32) >= 2 * 128 * 128 * 4
+
+
+def bytes_asked(call, t, r, c, px=0, py=0, dtype=binding.DTYPE_BF16):
+    """What one linear call asks for, from its refusal of a workspace of one byte. The pointers are made up: only where
+    nothing can be launched."""
+    if torch.cuda.is_available():
+        pytest.skip("made-up pointers")
+    at = lambda i: (1 << 40) + i * (1 << 36)  # noqa: E731
+    opt = binding.LayerOptions()
+    binding.load().dion2_layer_options_init(ctypes.byref(opt))
+    opt.dtype, opt.ld_x, opt.ld_dy, opt.workspace, opt.workspace_bytes = dtype, c + px, r + py, at(9), 1
+    lib = binding.load()
+    args = {"forward": (lib.dion2_linear_forward, (at(0), at(1), at(2), None, None, None)),
+            "input": (lib.dion2_linear_backward_input, (at(0), at(1), at(2), None)),
+            "weight": (lib.dion2_linear_backward_weight, (at(0), None, at(1), at(2)))}[call]
+    status = args[0](*args[1], t, r, c, ctypes.byref(opt), None)
+    assert status == binding.DION2_ERR_WORKSPACE, (status, binding.dion2_last_error())
+    return int(re.search(r"below the (\d+) needed", binding.dion2_last_error()).group(1))
+
+
+def copy_of(rows, width, e=2):
+    return -(-rows * -(-width * e // 16) * 16 // 256) * 256
+
+
+# (tokens, rows, cols, how much longer than its width a row of X and of dY is, call, what is copied, parts): calls of
+# test_gpu_layers_forms.py that run on copies in bf16, on tiles of 64, 128 and 256, whole and in parts
+COPIED = [(1500, 1001, 1003, 0, 0, "forward", "XW", 0), (1500, 1001, 1003, 0, 0, "input", "YW", 0),
+          (1500, 1001, 1003, 0, 0, "weight", "YX", 0), (2500, 2051, 1027, 0, 0, "forward", "XW", 0),
+          (8191, 2047, 2041, 0, 0, "forward", "XW", 0), (8191, 2047, 2041, 0, 0, "input", "YW", 0),
+          (8191, 2047, 2041, 0, 0, "weight", "YX", 2), (3000, 2048, 8192, 3, 5, "forward", "X", 2)]
+
+
+@pytest.mark.parametrize("t,r,c,px,py,call,copied,parts", COPIED)
+def test_bf16_copies_are_made_and_counted(t, r, c, px, py, call, copied, parts):
+    """The bytes asked for are the copies' and the parts' to the byte, and within what is said to suffice."""
+    want = sum({"X": copy_of(t, c), "Y": copy_of(t, r), "W": copy_of(r, c)}[k] for k in copied)
+    m, n = {"forward": (t, r), "input": (t, c), "weight": (r, c)}[call]
+    want += parts * -(-m // 32) * -(-n // 32) * 4096
+    got = bytes_asked(call, t, r, c, px, py)
+    assert got <= want + 255 and got >= want
+    assert got <= binding.dion2_linear_workspace_size(t, r, c, BF, ld_x=c + px, ld_dy=r + py)
