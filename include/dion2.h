@@ -417,8 +417,8 @@ int dion2_plan_form(int batch, int64_t rows, int64_t cols, float alpha,
  * touched, and gradients of parameters are sums of nothing.
  *
  * Numerical contract:
- *   - Every sum (products, means, column sums) is held in fp32 and an output
- *     is rounded once, to nearest even, from it. Products of bf16 operands
+ *   - Every sum (products, mean squares, column sums) is held in fp32, a row's
+ *     mean in 64 bits, and an output is rounded once, to nearest even, from it. Products of bf16 operands
  *     run on bf16 MFMA (exact products), those of fp32 operands on fp32 MFMA.
  *   - Sums are taken in an order fixed by the sizes, the type and whether
  *     pointers and pitches allow 16-byte loads: runs repeat bitwise. No atomics.

@@ -14,29 +14,40 @@ namespace {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ float wave_sum(float v) {
+template <typename V>
+__device__ __forceinline__ V wave_sum(V v) {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
     return v;
 }
-// Sum over the block in every thread; `red` holds one float a wave.
-__device__ __forceinline__ float block_sum(float v, float* red) {
+// Sum over the waves of a block in every thread; `red` holds one value a wave.
+// Calls in turn use two of them in turn, so one barrier a call is enough.
+template <int WAVES, typename V>
+__device__ __forceinline__ V block_sum(V v, V* red) {
     v = wave_sum(v);
-    __syncthreads();   // red's last use is over
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float s = 0.0f;
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) s += red[w];
-    return s;
+        for (int w = 0; w < WAVES; ++w) v += red[w];
+    }
+    return v;
 }
 
-// From the mean square deviation about a rounded mean and that mean's error,
-// which rounding can leave a little below 0 (a NaN stays one).
-__device__ __forceinline__ float variance(float d2, float off) {
-    const float v = d2 - off * off;
-    return v < 0.0f ? 0.0f : v;
-}
+// A row's mean, summed in 64 bits, as the nearest float and what that leaves: a
+// mean many times the row's spread then costs its deviations nothing, and what is
+// stored is the mean rounded once. (Deviations from a rounded mean, summed in 32
+// bits to correct it, round alike wherever the entries have few bits: on rows of
+// bf16 that mean was off by up to 1.8e-6 relative where a plain sum has 5e-8.)
+struct Mean {
+    float mean, off;
+    __device__ __forceinline__ Mean(double sum, int64_t cols) {
+        const double m = sum / (double)cols;
+        mean = (float)m;
+        off = __builtin_isfinite(mean) ? (float)(m - (double)mean) : 0.0f;
+    }
+};
 
 __device__ __forceinline__ int part8(int64_t n, int64_t at) { return n - at < 8 ? (int)(n - at) : 8; }
 
@@ -157,8 +168,8 @@ template <typename T, int WPR, int CH, bool RAGGED>
 __global__ __launch_bounds__(64 * row_waves(WPR)) void norm_regs(NormArgs a) {
     using R = Row<T, WPR, CH, RAGGED>;
     constexpr int RPB = row_waves(WPR) / WPR;   // rows a block
-    __shared__ float red[4 * WPR];
-    int turn = 0;
+    __shared__ double red[WPR];
+    __shared__ float red2[WPR];
     const int cols = (int)a.cols;
     const float inv = 1.0f / (float)cols;
     // a row a wave, or a block; the grid has a second dimension because a
@@ -167,17 +178,16 @@ __global__ __launch_bounds__(64 * row_waves(WPR)) void norm_regs(NormArgs a) {
     if (t >= a.tokens) return;   // whole waves, or the whole block
     R x;
     x.load(static_cast<const T*>(a.X) + t * a.ldx, cols);
-    float s = 0.0f, none = 0.0f, v[8];
+    double sum = 0.0;
+    float v[8];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         x.raw[i].get(v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s += v[j];
+        for (int j = 0; j < 8; ++j) sum += (double)v[j];
     }
-    row_sums<WPR>(s, none, red, turn);
-    const float mean = s * inv;
-    // the deviations' own mean takes up what rounding left of the mean
-    float d1 = 0.0f, d2 = 0.0f;
+    const Mean m(block_sum<WPR>(sum, red), cols);
+    float d2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int n = R::have(i, cols);
@@ -185,14 +195,11 @@ __global__ __launch_bounds__(64 * row_waves(WPR)) void norm_regs(NormArgs a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < n) {
-                const float d = v[j] - mean;
-                d1 += d;
+                const float d = v[j] - m.mean - m.off;
                 d2 += d * d;
             }
     }
-    row_sums<WPR>(d1, d2, red, turn);
-    const float off = d1 * inv;
-    const float rstd = 1.0f / sqrtf(variance(d2 * inv, off) + a.eps);
+    const float rstd = 1.0f / sqrtf(block_sum<WPR>(d2, red2) * inv + a.eps);
     T* y = static_cast<T*>(a.Y) + t * a.ldy;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
@@ -201,7 +208,7 @@ __global__ __launch_bounds__(64 * row_waves(WPR)) void norm_regs(NormArgs a) {
         float g[8];
         x.raw[i].get(v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = (v[j] - mean - off) * rstd;
+        for (int j = 0; j < 8; ++j) v[j] = (v[j] - m.mean - m.off) * rstd;
         if (a.gamma) {
             load8_as(a.gamma, c, a.p_bf16, RAGGED ? n : 8, g);
 #pragma unroll
@@ -215,7 +222,7 @@ __global__ __launch_bounds__(64 * row_waves(WPR)) void norm_regs(NormArgs a) {
         store8(y + c, RAGGED ? n : 8, v);
     }
     if ((threadIdx.x & 63) == 0 && threadIdx.x / 64 % WPR == 0) {
-        if (a.mean) stg(a.mean + t, mean + off);
+        if (a.mean) stg(a.mean + t, m.mean);
         if (a.rstd) stg(a.rstd + t, rstd);
     }
 }
@@ -361,37 +368,36 @@ __global__ __launch_bounds__(64 * row_waves(WPR), 4) void norm_grad_regs(NormGra
 // One block a row, the row read once per pass.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_rows(NormArgs a) {
-    __shared__ float red[kThreads / 64];
+    __shared__ double red[kThreads / 64];
+    __shared__ float red2[kThreads / 64];
     for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x) {
         const T* x = static_cast<const T*>(a.X) + t * a.ldx;
         T* y = static_cast<T*>(a.Y) + t * a.ldy;
-        float v[8], s = 0.0f;
+        float v[8];
+        double sum = 0.0;
         for (int64_t c = threadIdx.x * 8; c < a.cols; c += kThreads * 8) {
             load8(x + c, part8(a.cols, c), v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += v[i];
+            for (int i = 0; i < 8; ++i) sum += (double)v[i];
         }
-        const float n = (float)a.cols;
-        float mean = block_sum(s, red) / n;
-        float d1 = 0.0f, d2 = 0.0f;   // as in norm_regs
+        const Mean m(block_sum<kThreads / 64>(sum, red), a.cols);
+        float d2 = 0.0f;
         for (int64_t c = threadIdx.x * 8; c < a.cols; c += kThreads * 8) {
             const int k = part8(a.cols, c);
             load8(x + c, k, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = i < k ? v[i] - mean : 0.0f;
-                d1 += d;
+                const float d = i < k ? v[i] - m.mean - m.off : 0.0f;
                 d2 += d * d;
             }
         }
-        const float off = block_sum(d1, red) / n;
-        const float rstd = 1.0f / sqrtf(variance(block_sum(d2, red) / n, off) + a.eps);
+        const float rstd = 1.0f / sqrtf(block_sum<kThreads / 64>(d2, red2) / (float)a.cols + a.eps);
         for (int64_t c = threadIdx.x * 8; c < a.cols; c += kThreads * 8) {
             const int k = part8(a.cols, c);
             float g[8];
             load8(x + c, k, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = (v[i] - mean - off) * rstd;
+            for (int i = 0; i < 8; ++i) v[i] = (v[i] - m.mean - m.off) * rstd;
             if (a.gamma) {
                 load8_as(a.gamma, c, a.p_bf16, k, g);
 #pragma unroll
@@ -405,7 +411,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows(NormArgs a) {
             store8(y + c, k, v);
         }
         if (threadIdx.x == 0) {
-            if (a.mean) stg(a.mean + t, mean + off);
+            if (a.mean) stg(a.mean + t, m.mean);
             if (a.rstd) stg(a.rstd + t, rstd);
         }
     }
@@ -413,7 +419,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows(NormArgs a) {
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_grad_rows(NormGradArgs a) {
-    __shared__ float red[kThreads / 64];
+    __shared__ float red[2][kThreads / 64];
     for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x) {
         const T* x = static_cast<const T*>(a.X) + t * a.ldx;
         const T* dy = static_cast<const T*>(a.dY) + t * a.lddy;
@@ -442,8 +448,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_rows(NormGradArgs a) {
                     s2 += h[i] * xh[i];
                 }
         }
-        s1 = block_sum(s1, red) / (float)a.cols;
-        s2 = block_sum(s2, red) / (float)a.cols;
+        s1 = block_sum<kThreads / 64>(s1, red[0]) / (float)a.cols;
+        s2 = block_sum<kThreads / 64>(s2, red[1]) / (float)a.cols;
         for (int64_t c = threadIdx.x * 8; c < a.cols; c += kThreads * 8) {
             const int k = part8(a.cols, c);
             load(c, k);
