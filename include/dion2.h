@@ -420,8 +420,9 @@ int dion2_plan_form(int batch, int64_t rows, int64_t cols, float alpha,
  *   - Every sum (products, mean squares, column sums) is held in fp32, a row's
  *     mean in 64 bits, and an output is rounded once, to nearest even, from it. Products of bf16 operands
  *     run on bf16 MFMA (exact products), those of fp32 operands on fp32 MFMA.
- *   - Sums are taken in an order fixed by the sizes, the type and whether
- *     pointers and pitches allow 16-byte loads: runs repeat bitwise. No atomics.
+ *   - Sums are taken in an order fixed by the sizes, the types, the pitches, the
+ *     alignment of the pointers and which outputs are asked for (dbias with G and
+ *     dbias alone can differ in their last bits): runs repeat bitwise. No atomics.
  *   - Activations are evaluated in fp32, GELU's Phi(-|z|) within 1.5e-6 relative
  *     for |z| <= 4, 5e-6 for |z| <= 9 and 1e-5 for |z| <= 12 (beyond, it is
  *     below 2e-33 and so is what it is off by), from Z's sums before rounding
@@ -534,7 +535,8 @@ size_t dion2_layernorm_workspace_size(int64_t tokens, int64_t cols,
                                       const dion2_layer_options* opt);
 
 /* ---- Measurement hooks ---------------------------------------------------
- * While enabled, every kernel phase of subsequent calls is bracketed by HIP
+ * They time steps; layer calls record nothing and are not in the totals.
+ * While enabled, every kernel phase of subsequent steps is bracketed by HIP
  * events recorded on the call's stream (the Newton-Schulz s x s products of
  * the GRAM form, which run back to back, as one span), and the phase's
  * algorithmic work is added to per-phase totals, as flops and as bytes:

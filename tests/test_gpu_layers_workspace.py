@@ -49,3 +49,19 @@ def test_layer_calls_leave_a_captured_step_its_workspace(hip_device):
         a, b = dY.double().t().contiguous(), X.double()
         want, off = a @ b, (t + 16) * 2.0 ** -23 * (a.abs() @ b.abs())     # fp32 sums of t exact products, then one rounding
         assert bool(((out.double() - want).abs() <= off + 2.0 ** -24 * (want.abs() + off)).all())
+
+
+def test_layer_calls_are_not_in_the_steps_measured_phases(hip_device):
+    """The measurement hooks time steps: layer calls leave their totals at nothing."""
+    X, W = torch.ones((40, 64), dtype=BF, device="cuda"), torch.ones((96, 64), dtype=BF, device="cuda")
+    Y = torch.empty((40, 96), dtype=BF, device="cuda")
+    before = binding.dion2_profile_enable(True)
+    try:
+        binding.dion2_profile_reset()
+        binding.dion2_linear_forward(Y, X, W)
+        binding.dion2_layernorm_forward(X, X)
+        totals = binding.dion2_profile_read()
+    finally:
+        binding.dion2_profile_enable(before)
+        binding.dion2_profile_reset()
+    assert all(v["calls"] == 0 and v["launches"] == 0 and v["ms"] == 0 for v in totals.values())
