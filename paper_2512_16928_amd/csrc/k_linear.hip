@@ -1174,15 +1174,15 @@ double time_of(const Cost& c, const ProductArgs& a, int splits, double slow) {
 }
 
 // Copies cost a launch and their bytes at 4 TB/s. Forward, input and weight
-// gradient of 8191 tokens through 2047 x 2041: 78, 75 and 103 us with copies, on
+// gradient of 8191 tokens through 2047 x 2041: 77, 76 and 107 us with copies, on
 // tiles of any alignment 144, 202 and 284; 1531 tokens through 1000 x 517: 12.5,
 // 10.6, 13.3 and 10.3, 18.7, 16.4, in fp32 30, 28, 36 and 32, 35, 39.
 // Beyond kCopiesMost they would hold more memory than that time is worth.
 constexpr size_t kCopiesMost = size_t(2) << 30;
 // Parts are for few output tiles: on 512 of 256 x 256 (two rounds) four of them
-// are 512 MiB. More is refused, and so is a cut that by the model gains less than a
-// twentieth over the same tiles' whole sums, well inside what it is off by: 262144 tokens through 32000 x 8192 would
-// take 4 GB of parts for 0.02% of their 98 ms.
+// are 512 MiB. More is refused, and so is a cut that by the model gains less than
+// a twentieth over the same tiles' whole sums, well inside what it is off by:
+// 262144 tokens through 32000 x 8192 would take 4 GB of parts for 0.02% of 98 ms.
 constexpr size_t kPartsMost = size_t(512) << 20;
 constexpr double kPartsWorth = 1.05;
 constexpr int64_t kNearTiles = 1 << 16;   // none of its wins has more, and a launch takes them
